@@ -46,7 +46,9 @@ typedef enum tman_status {
     TMAN_ERR_WORKSPACE = -5, /* workspace missing or smaller than the *_workspace_bytes query */
     TMAN_ERR_ALIGN = -6,     /* a pointer is not 16-byte aligned */
     TMAN_ERR_LAUNCH = -7,    /* the HIP runtime reported an error when launching */
-    TMAN_ERR_HEADER = -8     /* a packed blob's header disagrees with the shape it is used with */
+    TMAN_ERR_HEADER = -8,    /* a packed blob's header disagrees with the shape it is used with */
+    TMAN_ERR_CACHE = -9,     /* element type, head size or page size of a key-value cache not supported */
+    TMAN_ERR_INDEX = -10     /* device status: a length, page or position in device memory was out of range */
 } tman_status;
 
 #define TMAN_FLAG_HAS_ZERO 1 /* weights carry a per-group zero point (affine form) */
@@ -399,6 +401,141 @@ typedef struct tman_tiling {
 int tman_default_tiling(tman_tiling_t *out);
 int tman_get_tiling(tman_tiling_t *out);
 int tman_set_tiling(const tman_tiling_t *tiling);
+
+/*
+ * Key-value cache in pages, and the operators around it: what stands between the fused QKV product and the O product of
+ * a decoder layer.  Inference only (no gradients).
+ *
+ * A cache is a pool of pages, each `page` positions of all key-value heads, keys and values apart:
+ *   k_pages, v_pages : [n_pages][kv_heads][page][dim], fp16 or bf16, 16-byte aligned
+ *   page_table       : int32 [n_seqs][max_pages], the pages of every sequence in order; position j of sequence b lies in
+ *                      page page_table[b][j / page] at j % page.  Entries past a sequence's length are not used.
+ * dim is 64, 128 or 256; page a power of two from 16 to 1024; max_pages * page at most 2^30 (the pool itself may be
+ * larger than 4 GiB).  q, k, v and outputs are [tokens][heads][dim] with the distance between tokens (in elements, a multiple
+ * of 8) given, so they may be columns of one fused matrix; 16-byte aligned.  Accumulated weights (`weights`), where given, are
+ * fp32 [n_pages][kv_heads][page], 16-byte aligned.
+ *
+ * New tokens of several sequences lie one after another: those of sequence b are rows q_start[b] to q_start[b + 1] - 1
+ * (q_start int32 [n_seqs + 1], ascending from 0, at most n_tokens), and they are the LAST positions of it: lens[b] (int32)
+ * counts them.  A sequence may have none.
+ *
+ * Lengths, tables and positions are read on the device.  One that is out of range (a length beyond the table or beyond
+ * max_len, a page that the pool has not) never leads out of the buffers: it is cut to the range (an appended token whose place
+ * does not exist is dropped), and tman_device_status returns TMAN_ERR_INDEX.
+ *
+ * Softmax statistics, sums and weights are fp32; the probabilities are rounded to the element type before they meet the
+ * values, as the matrix cores take them.  Deterministic: no floating-point atomics, the joins have a fixed order.
+ */
+#define TMAN_TYPE_F16 0
+#define TMAN_TYPE_BF16 1
+
+typedef struct tman_kv_cache {
+    void *k_pages;
+    void *v_pages;
+    const int32_t *page_table;
+    int32_t n_pages;
+    int32_t n_seqs;
+    int32_t max_pages; /* entries of a row of page_table */
+    int32_t kv_heads;
+    int32_t page; /* positions a page */
+    int32_t dim;  /* of a head */
+    int32_t type; /* TMAN_TYPE_* */
+} tman_kv_cache_t;
+
+/*
+ * Rotary positions: pair p of a head, 0 <= p < rot / 2, turns by the angle that the table holds for position
+ * P = positions[axis(p)][n] of token n:  (a, b) -> (a cos - b sin, a sin + b cos).
+ *   cos_sin     : fp32 [n_pos][rot / 2][2], 16-byte aligned
+ *   rot         : rotated coordinates of a head, a multiple of 16, at most dim; the rest is copied
+ *   axes        : 1 to 3 axes of positions (time, height, width); the first sections[0] pairs turn with axis 0, the next
+ *                 sections[1] with axis 1, ...; the sections add up to rot / 2
+ *   interleaved : 0: pair p is coordinates (p, p + rot / 2), 1: coordinates (2p, 2p + 1)
+ */
+typedef struct tman_rope {
+    const float *cos_sin;
+    int32_t n_pos;
+    int32_t rot;
+    int32_t axes;
+    int32_t sections[3];
+    int32_t interleaved;
+} tman_rope_t;
+
+/*
+ * Rotates q and k and writes k and v of n_tokens new tokens into the cache.
+ *   q, q_out  : [n_tokens][heads][dim] (q_stride, q_out_stride between tokens); q may be q_out; both NULL: no queries
+ *   k, v      : [n_tokens][kv_heads][dim] (kv_stride between tokens)
+ *   positions : int32 [axes][n_tokens]; NULL: every axis takes the token's position in its sequence
+ *   rope      : NULL: nothing is rotated
+ *   weights   : NULL, or the accumulated weights, which become zero for the new positions
+ *   q_start   : NULL: one token a sequence (n_tokens = n_seqs)
+ */
+int tman_rope_append(const tman_kv_cache_t *cache, const tman_rope_t *rope, int32_t heads, int32_t n_tokens, const void *q,
+                     int64_t q_stride, const void *k, const void *v, int64_t kv_stride, const int32_t *positions,
+                     const int32_t *q_start, const int32_t *lens, void *q_out, int64_t q_out_stride, float *weights,
+                     void *stream);
+
+/*
+ * How scores are made.  For a query at position i and a key at position j, of query head h and key-value head
+ * h / (heads / kv_heads):
+ *   s = scale * (q . k);   cap > 0: s = cap * tanh(s / cap);   slopes: s -= slopes[h] * |i - j|
+ * and window > 0 hides the keys with j <= i - window.  slopes: fp32 [heads] in device memory or NULL.
+ */
+typedef struct tman_attn {
+    int32_t heads; /* of queries, a multiple of kv_heads */
+    int32_t window;
+    float scale;
+    float cap;
+    const float *slopes;
+} tman_attn_t;
+
+/*
+ * Attention of one new token of every sequence over its cache: q, out [n_seqs][heads][dim]; the token is position
+ * lens[b] - 1 and sees positions first[b] (NULL: 0) to lens[b] - 1 (the keys and values of its own position are in the cache
+ * already).  A sequence that sees nothing (length zero, first at or behind the length) gives zeros.
+ *   max_len   : no sequence is longer (it sizes the launch; a tight bound makes the call faster)
+ *   lse       : NULL or fp32 [n_seqs][heads], log(sum exp(s)); minus infinity where nothing is seen
+ *   weights   : NULL or the accumulated weights: to those of every position that is seen the sum of its probabilities over the
+ *               query heads of the key-value head is added (pages then must not be shared between sequences)
+ *   workspace : at least tman_attn_decode_workspace_bytes for the same cache, attn and `weights` and max_len or more; 16-byte
+ *               aligned, zero-filled once before its first use.  Its tickets are back at zero after every call, so one
+ *               workspace serves calls of any sizes that fit it, of this function and of tman_attn_prefill; calls that may
+ *               overlap in time need workspaces of their own
+ */
+size_t tman_attn_decode_workspace_bytes(const tman_kv_cache_t *cache, const tman_attn_t *attn, int32_t max_len, int32_t weights);
+int tman_attn_decode(const tman_kv_cache_t *cache, const tman_attn_t *attn, const void *q, int64_t q_stride,
+                     const int32_t *lens, const int32_t *first, int32_t max_len, void *out, int64_t out_stride, float *lse,
+                     float *weights, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention of the new tokens of prompts (or chunks of prompts) over the cache, which holds their keys and values already
+ * (tman_rope_append): q, out [n_tokens][heads][dim].  Token n at position i of its sequence sees positions first[n] <= j <
+ * end[n] (NULL: 0 and i + 1; both are cut to the sequence's length), which says
+ *   causal            first = NULL, end = NULL
+ *   packed documents  first[n] = the start of n's document
+ *   a prefix          end[n] = max(i + 1, length of the prefix): seen by all, also by the tokens inside
+ * or any other interval.  A token that sees nothing gives zeros, and minus infinity in lse (fp32 [n_tokens][heads] or NULL).
+ * Hidden keys and values never reach a result, whatever they hold (infinities and NaN too).
+ *   workspace : at least tman_attn_prefill_workspace_bytes for the same cache, attn and n_tokens and for max_len or more (0:
+ *               NULL will do); as for tman_attn_decode
+ *   max_len   : no sequence is longer
+ */
+size_t tman_attn_prefill_workspace_bytes(const tman_kv_cache_t *cache, const tman_attn_t *attn, int32_t n_tokens, int32_t max_len);
+int tman_attn_prefill(const tman_kv_cache_t *cache, const tman_attn_t *attn, int32_t n_tokens, const void *q, int64_t q_stride,
+                      const int32_t *q_start, const int32_t *lens, const int32_t *first, const int32_t *end, int32_t max_len,
+                      void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Makes room: of every sequence longer than `keep` and every key-value head the `recent` last positions and, of the others, the
+ * keep - recent with the largest accumulated weights stay (equal weights: the lower position; NaN counts as larger than
+ * all), in their order.  They are copied to the pages of new_table, with their weights; shorter sequences are copied whole.
+ *   new_table : int32 [n_seqs][new_max_pages], new_max_pages * page >= keep; its pages are none that page_table uses
+ *   new_lens  : int32 [n_seqs], receives min(lens[b], keep)
+ *   kept      : int32 [n_seqs][kv_heads][keep], receives the kept positions, ascending (-1 behind the last of a short one)
+ * Heads keep positions of their own, so afterwards a position is an index into the head's cache: distances and windows count
+ * what was kept.  0 <= recent <= keep, keep >= 1, max_len as above.
+ */
+int tman_kv_evict(const tman_kv_cache_t *cache, float *weights, const int32_t *lens, int32_t keep, int32_t recent, int32_t max_len,
+                  const int32_t *new_table, int32_t new_max_pages, int32_t *new_lens, int32_t *kept, void *stream);
 
 /* Static, human-readable name of a status code. */
 const char *tman_status_string(int status);

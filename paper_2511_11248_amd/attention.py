@@ -1,0 +1,216 @@
+"""ctypes binding of the key-value cache's operators (see include/tman.h): a cache in pages, the rotation and append of new
+tokens, attention of single tokens and of prompts, and eviction by accumulated weight.
+
+Argument marshalling only.  Sizes and strides come from the tensors; a tensor that cannot be what the call takes (type, number of
+dimensions, heads that are not contiguous) raises ``TmanError`` before the library is called, everything else is checked there.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+from . import api
+from .api import TmanError, _check, _ptr, _stream
+
+TMAN_TYPE_F16, TMAN_TYPE_BF16 = 0, 1
+_ERR_NULL, _ERR_SHAPE, _ERR_CACHE = -1, -4, -9
+
+
+class _CCache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p), ("n_pages", C.c_int32),
+                ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("kv_heads", C.c_int32), ("page", C.c_int32),
+                ("dim", C.c_int32), ("type", C.c_int32)]
+
+
+class _CRope(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("n_pos", C.c_int32), ("rot", C.c_int32), ("axes", C.c_int32),
+                ("sections", C.c_int32 * 3), ("interleaved", C.c_int32)]
+
+
+class _CAttn(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p)]
+
+
+_types = None
+
+
+def _type_of(dtype) -> int:
+    global _types
+    if _types is None:
+        import torch
+
+        _types = {torch.float16: TMAN_TYPE_F16, torch.bfloat16: TMAN_TYPE_BF16}
+    return _types.get(dtype, -1)
+
+
+def _wants(ok: bool, where: str, status: int = _ERR_SHAPE) -> None:
+    if not ok:
+        raise TmanError(status, where)
+
+
+def _is(t, name: str) -> bool:
+    return str(t.dtype) == name and t.is_contiguous()
+
+
+_functions = None
+
+
+def _load():
+    global _functions
+    if _functions is None:
+        L = api._load()
+        vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+        L.tman_rope_append.restype = C.c_int
+        L.tman_rope_append.argtypes = [vp, vp, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, vp, vp]
+        L.tman_attn_decode_workspace_bytes.restype = sz
+        L.tman_attn_decode_workspace_bytes.argtypes = [vp, vp, i32, i32]
+        L.tman_attn_decode.restype = C.c_int
+        L.tman_attn_decode.argtypes = [vp, vp, vp, i64, vp, vp, i32, vp, i64, vp, vp, vp, sz, vp]
+        L.tman_attn_prefill_workspace_bytes.restype = sz
+        L.tman_attn_prefill_workspace_bytes.argtypes = [vp, vp, i32, i32]
+        L.tman_attn_prefill.restype = C.c_int
+        L.tman_attn_prefill.argtypes = [vp, vp, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, vp, vp, sz, vp]
+        L.tman_kv_evict.restype = C.c_int
+        L.tman_kv_evict.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp]
+        _functions = L
+    return _functions
+
+
+class KvCache:
+    """``tman_kv_cache_t`` over tensors: k_pages, v_pages [n_pages][kv_heads][page][dim] (fp16 or bf16, contiguous), page_table
+    int32 [n_seqs][max_pages].  Keeps the tensors alive; holds no state of its own."""
+
+    def __init__(self, k_pages, v_pages, page_table):
+        where = "KvCache"
+        _wants(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.is_contiguous() and v_pages.is_contiguous(), where)
+        kind = _type_of(k_pages.dtype)
+        _wants(kind >= 0 and v_pages.dtype == k_pages.dtype, where, _ERR_CACHE)
+        _wants(page_table.dim() == 2 and _is(page_table, "torch.int32"), where)
+        self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
+        n_pages, self.kv_heads, self.page, self.dim = k_pages.shape
+        self.n_seqs, self.max_pages = page_table.shape
+        self.dtype, self.n_pages = k_pages.dtype, n_pages
+        self._c = _CCache(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), n_pages, self.n_seqs, self.max_pages, self.kv_heads,
+                          self.page, self.dim, kind)
+        self._ref = C.byref(self._c)
+
+    def _rows(self, t, where: str, heads: int = 0) -> int:
+        """Stride between tokens of t [tokens][heads][dim], whose heads must be contiguous."""
+        _wants(t is not None, where, _ERR_NULL)
+        shape = t.shape
+        _wants(len(shape) == 3 and shape[2] == self.dim and (not heads or shape[1] == heads), where)
+        _wants(t.dtype == self.dtype, where, _ERR_CACHE)
+        stride, head, element = t.stride()
+        _wants(element == 1 and (head == self.dim or shape[1] == 1), where)
+        return stride if shape[0] > 1 else max(stride, shape[1] * self.dim)
+
+    def _weights(self, t, where: str) -> None:
+        _wants(t is None or (t.shape == self.k_pages.shape[:3] and _is(t, "torch.float32")), where)
+
+
+class Rope:
+    """``tman_rope_t``: cos_sin fp32 [n_pos][rot / 2][2]; sections: pairs per axis of positions (None: one axis)."""
+
+    def __init__(self, cos_sin, sections=None, interleaved: bool = False):
+        _wants(cos_sin.dim() == 3 and cos_sin.shape[2] == 2 and _is(cos_sin, "torch.float32"), "Rope")
+        self.cos_sin = cos_sin
+        pairs = cos_sin.shape[1]
+        self.sections = tuple(sections) if sections is not None else (pairs,)
+        _wants(1 <= len(self.sections) <= 3, "Rope")
+        self._c = _CRope(_ptr(cos_sin), cos_sin.shape[0], 2 * pairs, len(self.sections), (C.c_int32 * 3)(*self.sections),
+                         1 if interleaved else 0)
+        self._ref = C.byref(self._c)
+
+
+class Attn:
+    """``tman_attn_t``: how scores are made and what a window hides; slopes fp32 [heads] on the device or None."""
+
+    def __init__(self, heads: int, scale: float, cap: float = 0.0, window: int = 0, slopes=None):
+        _wants(slopes is None or (slopes.dim() == 1 and slopes.shape[0] == heads and _is(slopes, "torch.float32")), "Attn")
+        self.heads, self.scale, self.cap, self.window, self.slopes = heads, scale, cap, window, slopes
+        self._c = _CAttn(heads, window, scale, cap, _ptr(slopes))
+        self._ref = C.byref(self._c)
+
+
+def _ints(t, n: int, where: str, needed: bool = True) -> None:
+    _wants(t is not None or not needed, where, _ERR_NULL)
+    _wants(t is None or (t.numel() == n and _is(t, "torch.int32")), where)
+
+
+def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None, weights=None,
+                     stream=None) -> None:
+    """Rotates q and k (q_out may be q; both None: no queries) and writes k and v [n_tokens][kv_heads][dim] into the cache as the
+    last positions of their sequences; q_start None: one token a sequence."""
+    where = "tman_rope_append"
+    kv_stride = cache._rows(k, where, cache.kv_heads)
+    n = k.shape[0]
+    _wants(cache._rows(v, where, cache.kv_heads) == kv_stride and v.shape[0] == n, where)
+    heads = q_stride = q_out_stride = 0
+    if q is not None:
+        heads = q.shape[1]
+        q_stride = cache._rows(q, where)
+        q_out_stride = cache._rows(q_out, where, heads)
+        _wants(q.shape[0] == n and q_out.shape[0] == n, where)
+    _ints(lens, cache.n_seqs, where)
+    _ints(q_start, cache.n_seqs + 1, where, needed=False)
+    if positions is not None:
+        _wants(rope is not None, where)
+        _ints(positions, len(rope.sections) * n, where)
+    cache._weights(weights, where)
+    _check(_load().tman_rope_append(cache._ref, rope._ref if rope is not None else None, heads, n, _ptr(q), q_stride, _ptr(k), _ptr(v),
+                                    kv_stride, _ptr(positions), _ptr(q_start), _ptr(lens), _ptr(q_out), q_out_stride,
+                                    _ptr(weights), _stream(stream)), where)
+
+
+def tman_attn_decode_workspace_bytes(cache: KvCache, attn: Attn, max_len: int, weights: bool = False) -> int:
+    return int(_load().tman_attn_decode_workspace_bytes(cache._ref, attn._ref, max_len, 1 if weights else 0))
+
+
+def tman_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, workspace, first=None, lse=None, weights=None,
+                     stream=None) -> None:
+    """Attention of one new token of every sequence over its cache; the workspace is zero-filled once by the caller."""
+    where = "tman_attn_decode"
+    q_stride, out_stride = cache._rows(q, where, attn.heads), cache._rows(out, where, attn.heads)
+    B = cache.n_seqs
+    _wants(q.shape[0] == B and out.shape[0] == B, where)
+    _ints(lens, B, where)
+    _ints(first, B, where, needed=False)
+    _wants(lse is None or (lse.numel() == B * attn.heads and _is(lse, "torch.float32")), where)
+    cache._weights(weights, where)
+    _check(_load().tman_attn_decode(cache._ref, attn._ref, _ptr(q), q_stride, _ptr(lens), _ptr(first), max_len, _ptr(out), out_stride,
+                                    _ptr(lse), _ptr(weights), _ptr(workspace), 0 if workspace is None else api._nbytes(workspace),
+                                    _stream(stream)), where)
+
+
+def tman_attn_prefill_workspace_bytes(cache: KvCache, attn: Attn, n_tokens: int, max_len: int) -> int:
+    return int(_load().tman_attn_prefill_workspace_bytes(cache._ref, attn._ref, n_tokens, max_len))
+
+
+def tman_attn_prefill(cache: KvCache, attn: Attn, q, q_start, lens, out, max_len: int, workspace=None, first=None, end=None, lse=None,
+                      stream=None) -> None:
+    """Attention of the new tokens of prompts over the cache that holds them; token n sees positions first[n] <= j < end[n]."""
+    where = "tman_attn_prefill"
+    q_stride, out_stride = cache._rows(q, where, attn.heads), cache._rows(out, where, attn.heads)
+    n = q.shape[0]
+    _wants(out.shape[0] == n, where)
+    _ints(q_start, cache.n_seqs + 1, where)
+    _ints(lens, cache.n_seqs, where)
+    _ints(first, n, where, needed=False)
+    _ints(end, n, where, needed=False)
+    _wants(lse is None or (lse.numel() == n * attn.heads and _is(lse, "torch.float32")), where)
+    _check(_load().tman_attn_prefill(cache._ref, attn._ref, n, _ptr(q), q_stride, _ptr(q_start), _ptr(lens), _ptr(first), _ptr(end),
+                                     max_len, _ptr(out), out_stride, _ptr(lse), _ptr(workspace),
+                                     0 if workspace is None else api._nbytes(workspace), _stream(stream)), where)
+
+
+def tman_kv_evict(cache: KvCache, weights, lens, keep: int, recent: int, new_table, new_lens, kept, max_len: int, stream=None) -> None:
+    """Keeps `keep` positions of every sequence and key-value head (the `recent` last and the largest weights) in the pages of
+    new_table; new_lens [n_seqs] and kept [n_seqs][kv_heads][keep] receive the lengths and the positions that stayed."""
+    where = "tman_kv_evict"
+    _wants(weights is not None and new_table is not None, where, _ERR_NULL)
+    cache._weights(weights, where)
+    _ints(lens, cache.n_seqs, where)
+    _ints(new_lens, cache.n_seqs, where)
+    _ints(kept, cache.n_seqs * cache.kv_heads * keep, where)
+    _wants(new_table.dim() == 2 and new_table.shape[0] == cache.n_seqs and _is(new_table, "torch.int32"), where)
+    _check(_load().tman_kv_evict(cache._ref, _ptr(weights), _ptr(lens), keep, recent, max_len, _ptr(new_table), new_table.shape[1],
+                                 _ptr(new_lens), _ptr(kept), _stream(stream)), where)

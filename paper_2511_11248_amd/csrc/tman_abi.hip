@@ -485,6 +485,8 @@ const char* tman_status_string(int status) {
         case TMAN_ERR_ALIGN: return "pointer not 16-byte aligned";
         case TMAN_ERR_LAUNCH: return "HIP launch failed";
         case TMAN_ERR_HEADER: return "packed blob's header disagrees with the shape";
+        case TMAN_ERR_CACHE: return "element type, head size or page size of the cache not supported";
+        case TMAN_ERR_INDEX: return "a length, page or position in device memory is out of range";
         default: return "unknown status";
     }
 }

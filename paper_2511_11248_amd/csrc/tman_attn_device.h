@@ -1,0 +1,166 @@
+// Device functions shared by the kernels of the key-value cache's operators.
+#pragma once
+#include "tman_attn.h"
+
+namespace tman {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.402823466e38f;  // of a running maximum before the first score: finite, so differences with it are no NaN
+constexpr float kMinusInf = -__builtin_huge_valf();
+
+// Element types.  Operands of the matrix instructions travel as four 32-bit words of eight elements.
+struct F16 {
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {  // to nearest even, both
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, half2_t));
+    }
+    static __device__ __forceinline__ float low(uint32_t w) { return (float)__builtin_bit_cast(half2_t, w).x; }
+    static __device__ __forceinline__ float high(uint32_t w) { return (float)__builtin_bit_cast(half2_t, w).y; }
+    static constexpr uint32_t kExponent = 0x7c00u;  // bits that are all set in infinities and NaN
+};
+struct BF16 {
+    static __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8_t, a), __builtin_bit_cast(bf8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8_t, a), __builtin_bit_cast(bf8_t, b), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, bf2_t));
+    }
+    static __device__ __forceinline__ float low(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+    static __device__ __forceinline__ float high(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
+    static constexpr uint32_t kExponent = 0x7f80u;
+};
+
+template <typename T>
+using lds_pointer = T __attribute__((address_space(3)))*;
+template <typename T>
+__device__ __forceinline__ T lds_read(uint32_t at) {
+    return *reinterpret_cast<lds_pointer<const T>>(static_cast<uintptr_t>(at));
+}
+template <typename T>
+__device__ __forceinline__ void lds_write(uint32_t at, T v) {
+    *reinterpret_cast<lds_pointer<T>>(static_cast<uintptr_t>(at)) = v;
+}
+// Four rows of 16 elements to sixteen columns of four: lane i of each 16 gives the address of elements 4 (i % 4) .. + 3 of row i / 4 and
+// receives column i of rows 0 to 3.
+__device__ __forceinline__ u32x2 lds_read_columns(uint32_t at) {
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<lds_pointer<s16x4>>(static_cast<uintptr_t>(at))));
+}
+
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// A word that the whole wave reads, with a scalar load.
+__device__ __forceinline__ int scalar_load(const int32_t* p, int64_t i) {
+    return *(reinterpret_cast<const int32_t __attribute__((address_space(4)))*>(reinterpret_cast<uintptr_t>(p)) + i);
+}
+
+// max and sum of x over the lanes that differ in bit 5 (of two 32-lane halves), or in bits 4 and 5 (of four rows of 16)
+__device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+    return fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1]));
+}
+__device__ __forceinline__ float sum_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+    return __builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]);
+}
+__device__ __forceinline__ float max_rows(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+    return max_halves(fmaxf(__builtin_bit_cast(float, (int)r[0]), __builtin_bit_cast(float, (int)r[1])));
+}
+__device__ __forceinline__ float sum_rows(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(int, x), __builtin_bit_cast(int, x), false, false);
+    return sum_halves(__builtin_bit_cast(float, (int)r[0]) + __builtin_bit_cast(float, (int)r[1]));
+}
+
+__device__ __forceinline__ void report_index_error(int* status) {
+    __hip_atomic_store(status, (int)TMAN_ERR_INDEX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Length of sequence b, cut to what its table and the caller's bound hold.
+__device__ __forceinline__ int checked_length(const KvView& c, const int32_t* lens, int b, int max_len) {
+    const int n = scalar_load(lens, b);
+    const int most = min(max_len, c.max_pages << c.page_shift);
+    if ((unsigned)n <= (unsigned)most) return n;
+    report_index_error(c.status);
+    return n < 0 ? 0 : most;
+}
+// Pool index of entry `i` of sequence b's table, cut to the pool; one that is `used` and outside is reported.
+__device__ __forceinline__ int checked_page(const KvView& c, int b, int i, bool used) {
+    const int id = scalar_load(c.table, (int64_t)b * c.max_pages + min(i, c.max_pages - 1));
+    if ((unsigned)id < (unsigned)c.n_pages) return id;
+    if (used) report_index_error(c.status);
+    return 0;
+}
+// Where position j of a sequence's key-value head hk, in page `id`, lies in either pool: in rows of a head.
+__device__ __forceinline__ int64_t row_place(const KvView& c, int id, int hk, int j) {
+    return (((int64_t)id * c.kv_heads + hk) << c.page_shift) + (j & ((1 << c.page_shift) - 1));
+}
+
+// A raw buffer resource: what lies at or beyond `bytes` reads as zero.
+__device__ __forceinline__ u32x4 resource(const uint8_t* base, uint32_t bytes) {
+    const uint64_t at = reinterpret_cast<uintptr_t>(base);
+    return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+// One request of 64 x 16 bytes straight into LDS at `to` (the wave's lanes one after another).  Written out, since for the
+// builtin the compiler waits for ALL requests under way ahead of any read of LDS that it cannot tell apart from them; the
+// waits here are counted by hand.  It returns nothing in registers.  m0, a reserved register that cannot be named as overwritten, is
+// used by nothing else in these kernels (no builtin of this kind, no indexing of registers).
+__device__ __forceinline__ void request_to_lds(u32x4 rsrc, uint32_t offset, uint32_t scalar_offset, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(offset), "s"(rsrc), "s"(scalar_offset), "s"(to)
+                 : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_requests() {  // until at most N requests (of any kind, they end in order) are under way
+    static_assert(N >= 0 && N < 64, "what the counter holds");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Scores are made in units of log2: exp2 needs no product then.  raw = q . k.
+struct ScoreRule {
+    float scale;    // scale * log2 e, capped: 2 scale log2 e / cap
+    float cap;      // cap * log2 e, or 0
+    __device__ __forceinline__ ScoreRule(float s, float c) : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e) {}
+};
+// cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of 2^-23 cap, whatever x.
+template <bool CAP>
+__device__ __forceinline__ float score_of(float raw, const ScoreRule& r) {
+    if constexpr (!CAP) return raw * r.scale;
+    const float e = __builtin_amdgcn_exp2f(raw * r.scale);
+    return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap);
+}
+
+// Rows of keys and values in LDS.  A request (one wave, 64 x 16 bytes straight into LDS) brings 1024 bytes, whole rows; lane l's 16 bytes
+// land at 16 l of it, so an arrangement that keeps the reads off each other's banks is made by choosing which bytes a lane asks for:
+// chunk c (16 bytes) of row r is kept at place c ^ key_turn(r), or c ^ value_turn(r).
+template <int D>
+struct RowsOf {
+    static constexpr int kBytes = D * 2;
+    static constexpr int kRowsPerRequest = 1024 / kBytes;
+    // keys: 16 lanes read the same chunk of 16 consecutive rows; rows of 128 bytes share 256 bytes of banks by twos
+    static constexpr __host__ __device__ uint32_t key_turn(uint32_t r) { return D == 64 ? (r >> 1) & 7 : r & 15; }
+    // values, 16 columns of 4 rows for each 16 lanes: 32 bytes of each of 8 rows (32 lanes of a 16-column product) ...
+    static constexpr __host__ __device__ uint32_t value_turn(uint32_t r) { return (D == 64 ? (r >> 1) & 3 : r & 7) << 1; }
+    // ... or 64 bytes of each of 4 rows (of a 32-column product)
+    static constexpr __host__ __device__ uint32_t value_turn32(uint32_t r) { return (D == 64 ? (r >> 1) & 1 : r & 3) << 2; }
+};
+
+}  // namespace tman

@@ -1,0 +1,363 @@
+// Attention of the new tokens of prompts over a paged cache.
+//
+// What bounds it: the matrix cores, and beside them the vector pipe, which makes an exponential and about six other operations of
+// every score that the matrix cores spend 4 * dim operations on.
+//   * A workgroup takes 128 rows of one sequence and one key-value head - new tokens times the query heads of the group, so that
+//     the heads that share keys share the tiles of them - and walks over tiles of 64 positions, of which it sees an interval.
+//   * Keys and values of the next tile go straight into LDS while the present one is worked on (two buffers).
+//   * Scores are K q^T with a key a row and a query a column (32x32x16): a lane holds 32 scores of ONE query, so the softmax needs
+//     one exchange between two half waves, and the probabilities are, as they are, the operand of out^T = V^T P^T; V^T is
+//     read from LDS by columns in the same order of keys.
+//   * Only tiles in which some query of a wave does not see all keys compare positions.  There a hidden value may be anything,
+//     infinity and NaN included: such tiles are looked through, and what is not finite is left out of the products and added
+//     where it is seen.
+#include "tman_attn_device.h"
+
+namespace tman {
+namespace {
+
+constexpr int kTile = 64;  // positions
+constexpr int kWaves = 4, kThreads = kWaves * 64;
+constexpr int kTileRows = kWaves * 32;
+constexpr int kMaxSplit = 64;
+
+// [item][piece]: every wave's accumulators as they lie in its lanes, then its maxima and sums
+__host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kTileRows * D + 2 * kTileRows; }
+
+__device__ __forceinline__ void store_shared(float* p, float x, float y) {
+    const u32x2 w = {__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, w), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 load_shared(const float* p) {
+    return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+__device__ __forceinline__ int min_of_columns(int x) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) x = min(x, __shfl_xor(x, d));
+    return scalar(x);
+}
+
+// the elements of w that are not finite, as all ones
+template <class T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    constexpr uint32_t e = T::kExponent;
+    return ((w & e) == e ? 0xffffu : 0u) | ((w & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
+}
+
+template <class T, int D, bool CAP>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kernel(PrefillArgs a) {
+    using R = RowsOf<D>;
+    constexpr int kRowBytes = R::kBytes, kSlot = kTile * kRowBytes;      // of keys, and of values
+    constexpr int kOwnRows = kTile / kWaves;                            // rows that a wave requests of a tile: 16, in one page
+    constexpr int kRequests = kOwnRows * kRowBytes / 1024;              // and as many requests for the values
+    constexpr int kBlocks = D / 32;
+    __shared__ __attribute__((aligned(1024))) uint8_t room[2 * 2 * kSlot];
+    __shared__ int wave_lo[kWaves], wave_hi[kWaves], last;
+
+    const int wave = scalar((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int col = lane & 31, half = lane >> 5;
+
+    // which rows: the heaviest (the last) first, key-value heads over the XCDs
+    const int hk = (int)blockIdx.x % a.c.kv_heads, rest = (int)blockIdx.x / a.c.kv_heads;
+    const int piece = rest % a.p.n_split, item = a.p.row_tiles - 1 - rest / a.p.n_split;
+    int b = -1, tile = item, start = 0, tokens = 0;
+    for (int at = 0; at < a.c.n_seqs && b < 0; at += 64) {
+        int s0 = 0, n = 0;
+        if (at + lane < a.c.n_seqs) {
+            s0 = min(max(a.q_start[at + lane], 0), a.n_tokens);
+            n = min(max(a.q_start[at + lane + 1], s0), a.n_tokens) - s0;
+        }
+        const int tiles = (int)(((int64_t)n * a.group + kTileRows - 1) / kTileRows);
+        int run = tiles;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(run, d);
+            if (lane >= d) run += other;
+        }
+        const uint64_t found = __ballot(run > tile);
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            b = at + l;
+            tile -= __builtin_amdgcn_readlane(run - tiles, l);
+            start = __builtin_amdgcn_readlane(s0, l);
+            tokens = __builtin_amdgcn_readlane(n, l);
+        } else {
+            tile -= __builtin_amdgcn_readlane(run, 63);
+        }
+    }
+    if (b < 0) return;
+    const int len = checked_length(a.c, a.lens, b, a.max_len);
+    if (tokens > len && threadIdx.x == 0) report_index_error(a.c.status);
+
+    // the lane's row: a token and a query head, and the interval [lo, hi) that it sees
+    const int64_t row64 = (int64_t)tile * kTileRows + wave * 32 + col;
+    const bool valid = row64 < (int64_t)tokens * a.group;
+    const int row = valid ? (int)row64 : 0;
+    const int token = row / a.group, head = hk * a.group + row - token * a.group;
+    const int n = start + token, at = len - tokens + token;
+    int lo = 0, hi = at + 1;
+    if (a.first) lo = max(a.first[n], 0);
+    if (a.end) hi = a.end[n];
+    if (a.window > 0) lo = max(lo, at + 1 - a.window);
+    hi = min(hi, len);
+    const bool sees = valid && lo < hi;
+    // of the wave: everything that is seen lies in [least, most), what all see in [inner_lo, inner_hi)
+    const int least = min_of_columns(sees ? lo : 0x7fffffff), most = -min_of_columns(sees ? -hi : 0);
+    const int inner_lo = -min_of_columns(sees ? -lo : 0), inner_hi = min_of_columns(sees ? hi : 0x7fffffff);
+    if (lane == 0) {
+        wave_lo[wave] = least;
+        wave_hi[wave] = most;
+    }
+    __syncthreads();
+    int all_lo = 0x7fffffff, all_hi = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        all_lo = min(all_lo, scalar(wave_lo[w]));
+        all_hi = max(all_hi, scalar(wave_hi[w]));
+    }
+    const int first_tile = all_lo < all_hi ? all_lo / kTile : 0, n_tiles = all_lo < all_hi ? (all_hi + kTile - 1) / kTile - first_tile : 0;
+    const int per_piece = (n_tiles + a.p.n_split - 1) / a.p.n_split;
+    const int pieces = per_piece > 0 ? (n_tiles + per_piece - 1) / per_piece : 1;
+    if (piece >= pieces) return;
+    const int t0 = first_tile + piece * per_piece, t1 = min(first_tile + n_tiles, t0 + per_piece);
+
+    // queries: column col, coordinates 16 x + 8 half ..
+    u32x4 q[D / 16];
+    const u32x4* q_row = reinterpret_cast<const u32x4*>(a.q + (n * a.q_stride + (int64_t)head * D) * 2);
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) q[x] = q_row[2 * x + half];
+    const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    const bool sloped = a.slopes != nullptr;
+    const ScoreRule rule(a.scale, a.cap);
+
+    const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
+    const uint32_t in_row = lane % (kRowBytes / 16), ask_row = lane / (kRowBytes / 16);
+    const uint32_t k_ask = ask_row * kRowBytes + (in_row ^ R::key_turn(ask_row)) * 16;
+    const uint32_t v_ask = ask_row * kRowBytes + (in_row ^ R::value_turn32(ask_row)) * 16;
+    auto request = [&](int t, uint32_t to) {
+        const int j = t * kTile + wave * kOwnRows;
+        const int64_t place = row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
+        const u32x4 k = resource(a.c.k + place, kOwnRows * kRowBytes), v = resource(a.c.v + place, kOwnRows * kRowBytes);
+#pragma unroll
+        for (int i = 0; i < kRequests; ++i)
+            request_to_lds(k, k_ask ^ (R::key_turn(i * R::kRowsPerRequest) * 16), i * 1024, to + (wave * kRequests + i) * 1024);
+#pragma unroll
+        for (int i = 0; i < kRequests; ++i)
+            request_to_lds(v, v_ask ^ (R::value_turn32(i * R::kRowsPerRequest) * 16), i * 1024, to + kSlot + (wave * kRequests + i) * 1024);
+    };
+    // reads: keys of row 32 kb + col, chunk 2 x + half; values of rows .. + 4 half, columns 32 d + 16 (lane / 16 % 2) ..
+    const uint32_t k_read = col * kRowBytes, k_chunk = half ^ R::key_turn(col);
+    const int v_row = 4 * half + ((lane & 15) >> 2);
+    const uint32_t v_read = kSlot + v_row * kRowBytes + (lane & 1) * 8;
+    const uint32_t v_chunk = (((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) ^ R::value_turn32(v_row);
+
+    f32x16 out[kBlocks];
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d) out[d] = f32x16{};
+    float top = kLowest, sum = 0.f;
+
+    if (t0 < t1) request(t0, all);
+    for (int t = t0; t < t1; ++t) {
+        const uint32_t buffer = all + ((t - t0) & 1) * (2 * kSlot);
+        if (t + 1 < t1) {
+            request(t + 1, all + ((t + 1 - t0) & 1) * (2 * kSlot));
+            wait_requests<2 * kRequests>();
+        } else {
+            wait_requests<0>();
+        }
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int j0 = t * kTile;
+        if (j0 < most && j0 + kTile > least) {
+            const bool part = j0 < inner_lo || j0 + kTile > inner_hi;
+            f32x16 s[2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                s[kb] = f32x16{};
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x)
+                    s[kb] = T::mfma32(lds_read<u32x4>(buffer + k_read + kb * 32 * kRowBytes + (k_chunk ^ (2 * x)) * 16), q[x], s[kb]);
+            }
+            float best = kLowest;
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = j0 + 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
+                    float x = score_of<CAP>(s[kb][i], rule);
+                    if (sloped) x = __builtin_fmaf(-slope, fabsf((float)(at - j)), x);
+                    if (part) x = j >= lo && j < hi ? x : kMinusInf;
+                    s[kb][i] = x;
+                    best = fmaxf(best, x);
+                }
+            best = fmaxf(top, max_halves(best));
+            if (__any(best > top)) {
+                const float f = __builtin_amdgcn_exp2f(top - best);
+                sum *= f;
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d) out[d] *= f;
+                top = best;
+            }
+            u32x4 p[4];  // 16 keys each
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(s[kb][i] - top), e1 = __builtin_amdgcn_exp2f(s[kb][i + 1] - top);
+                    sum += e0 + e1;
+                    p[2 * kb + i / 8][i % 8 / 2] = T::pack(e0, e1);
+                }
+            bool odd_values = false;
+            if (part) {
+                uint32_t odd = 0;
+                for (int x = lane; x < kSlot / 16; x += 64) {
+                    const u32x4 w = lds_read<u32x4>(buffer + kSlot + x * 16);
+                    odd |= not_finite<T>(w.x) | not_finite<T>(w.y) | not_finite<T>(w.z) | not_finite<T>(w.w);
+                }
+                odd_values = __any(odd != 0);
+            }
+            if (!odd_values) {
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                    for (int d = 0; d < kBlocks; ++d) {
+                        const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
+                        const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
+                        out[d] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p[ks], out[d]);
+                    }
+            } else {
+                for (int ks = 0; ks < 4; ++ks) {
+                    const u32x4 pk = ks == 0 ? p[0] : ks == 1 ? p[1] : ks == 2 ? p[2] : p[3];
+#pragma unroll
+                    for (int d = 0; d < kBlocks; ++d) {
+                        const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
+                        const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
+                        out[d] = T::mfma32(u32x4{v0.x & ~not_finite<T>(v0.x), v0.y & ~not_finite<T>(v0.y), v1.x & ~not_finite<T>(v1.x),
+                                                 v1.y & ~not_finite<T>(v1.y)}, pk, out[d]);
+                    }
+                }
+                for (int y = 0; y < kTile; ++y) {
+                    const bool seen = j0 + y >= lo && j0 + y < hi;
+#pragma unroll
+                    for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t place = (4 * d + i) ^ R::value_turn32(y);
+                            const u32x2 w = lds_read<u32x2>(buffer + kSlot + y * kRowBytes + place * 16 + half * 8);
+                            const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
+                            if (seen && (m.x & 0xffffu)) out[d][4 * i] += T::low(w.x);
+                            if (seen && (m.x >> 16)) out[d][4 * i + 1] += T::high(w.x);
+                            if (seen && (m.y & 0xffffu)) out[d][4 * i + 2] += T::low(w.y);
+                            if (seen && (m.y >> 16)) out[d][4 * i + 3] += T::high(w.y);
+                        }
+                }
+            }
+        }
+        wait_lds();
+        __builtin_amdgcn_s_barrier();  // all have read this buffer
+        asm volatile("" ::: "memory");
+    }
+    sum = sum_halves(sum);
+
+    if (pieces > 1) {
+        // the pieces meet in the workspace; the last to arrive adds them up in their order
+        const int64_t group_item = (int64_t)item * a.c.kv_heads + hk;
+        float* base = a.partial + group_item * a.p.n_split * partial_floats(D);
+        const bool any = __any(valid);
+        if (any) {
+            float* mine = base + piece * partial_floats(D);
+#pragma unroll
+            for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2)
+                    store_shared(mine + (((wave * kBlocks + d) * 8 + i / 2) * 64 + lane) * 2, out[d][i], out[d][i + 1]);
+            if (half == 0) store_shared(mine + kTileRows * D + (wave * 32 + col) * 2, top, sum);
+        }
+        wait_requests<0>();
+        __syncthreads();
+        if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.tickets + group_item, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
+        __syncthreads();
+        if (!last) return;
+        if (threadIdx.x == 0) __hip_atomic_store(a.tickets + group_item, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (!any) return;
+        top = kLowest;
+        for (int p = 0; p < pieces; ++p) top = fmaxf(top, load_shared(base + p * partial_floats(D) + kTileRows * D + (wave * 32 + col) * 2).x);
+        sum = 0.f;
+#pragma unroll
+        for (int d = 0; d < kBlocks; ++d) out[d] = f32x16{};
+        for (int p = 0; p < pieces; ++p) {
+            const float* from = base + p * partial_floats(D);
+            const f32x2 ml = load_shared(from + kTileRows * D + (wave * 32 + col) * 2);
+            const float f = __builtin_amdgcn_exp2f(ml.x - top);
+            sum = __builtin_fmaf(f, ml.y, sum);
+#pragma unroll
+            for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) {
+                    const f32x2 v = load_shared(from + (((wave * kBlocks + d) * 8 + i / 2) * 64 + lane) * 2);
+                    out[d][i] = __builtin_fmaf(f, v.x, out[d][i]);
+                    out[d][i + 1] = __builtin_fmaf(f, v.y, out[d][i + 1]);
+                }
+        }
+    }
+
+    if (!valid) return;
+    const bool empty = !sees || sum == 0.f;
+    const float inv = empty ? 0.f : 1.f / sum;
+    uint8_t* to = a.out + (n * a.out_stride + (int64_t)head * D) * 2;
+#pragma unroll
+    for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u32x2 w = {T::pack(out[d][4 * i] * inv, out[d][4 * i + 1] * inv), T::pack(out[d][4 * i + 2] * inv, out[d][4 * i + 3] * inv)};
+            if (empty) w = u32x2{0, 0};
+            *reinterpret_cast<u32x2*>(to + (32 * d + 8 * i + 4 * half) * 2) = w;
+        }
+    if (a.lse && half == 0) a.lse[(int64_t)n * a.heads + head] = empty ? kMinusInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <class T, int D>
+void launch_of(const PrefillArgs& a, int grid, hipStream_t st) {
+    auto* kernel = a.cap > 0.f ? attn_prefill_kernel<T, D, true> : attn_prefill_kernel<T, D, false>;
+    kernel<<<grid, kThreads, 0, st>>>(a);
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+}  // namespace
+
+constexpr int kWantedWorkgroups = 512;  // two for each unit
+
+PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len) {
+    PrefillPlan p;
+    const int64_t rows = (int64_t)n_tokens * (a->heads / c->kv_heads);
+    // every sequence may leave one tile partly filled, and none has more than its rows
+    const int64_t tiles = rows / kTileRows + (c->n_seqs < n_tokens ? c->n_seqs : n_tokens), items = tiles * c->kv_heads;
+    int64_t pieces = items > kAttnTickets ? 1 : ceil_div(kWantedWorkgroups, items);
+    if (pieces > kMaxSplit) pieces = kMaxSplit;
+    if (pieces > ceil_div(max_len, 4 * kTile)) pieces = ceil_div(max_len, 4 * kTile);
+    if (pieces < 1) pieces = 1;
+    p.row_tiles = (int)tiles;
+    p.n_split = (int)pieces;
+    p.partial_at = kAttnTicketBytes;
+    p.bytes = pieces > 1 ? p.partial_at + items * pieces * partial_floats(c->dim) * sizeof(float) : 0;
+    return p;
+}
+
+int launch_attn_prefill(const PrefillArgs& a, hipStream_t st) {
+    const int64_t grid = (int64_t)a.p.row_tiles * a.p.n_split * a.c.kv_heads;
+    if (grid > 0x7fffffff) return TMAN_ERR_SHAPE;
+    if (a.c.type == TMAN_TYPE_F16) {
+        if (a.c.dim == 64) launch_of<F16, 64>(a, (int)grid, st);
+        else if (a.c.dim == 128) launch_of<F16, 128>(a, (int)grid, st);
+        else launch_of<F16, 256>(a, (int)grid, st);
+    } else {
+        if (a.c.dim == 64) launch_of<BF16, 64>(a, (int)grid, st);
+        else if (a.c.dim == 128) launch_of<BF16, 128>(a, (int)grid, st);
+        else launch_of<BF16, 256>(a, (int)grid, st);
+    }
+    return launch_status();
+}
+
+}  // namespace tman

@@ -1,0 +1,316 @@
+// What writes a paged cache (rotary positions and the append of new tokens) and what makes room in it (eviction by
+// accumulated attention weight).  All of it is bound by HBM: every element is read once and written once.
+#include "tman_attn_device.h"
+
+namespace tman {
+namespace {
+
+// ---- rotary positions and append
+//
+// A wave takes one token and a run of its head rows (queries, then keys, then values).  A unit of work is 16 elements of a
+// head: eight pairs that turn, or 16 elements that are copied; D / 16 lanes make a head, so a wave takes 1024 / D heads at once
+// and the angles of a lane's pairs are the same for all heads and are read once.
+constexpr int kAppendWaves = 4;
+
+template <class T>
+__device__ __forceinline__ void turn_pair(float& x, float& y, float c, float s) {
+    const float a = x, b = y;
+    x = __builtin_fmaf(a, c, -(b * s));
+    y = __builtin_fmaf(a, s, b * c);
+}
+
+template <class T, int D>
+__global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendArgs a) {
+    constexpr int kUnits = D / 16, kRows = 64 / kUnits;  // head rows a wave takes at once
+    const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
+    const int n = blockIdx.x;
+    const int unit = lane % kUnits, sub = lane / kUnits;
+    const int G = a.c.kv_heads, rows = a.heads + 2 * G;
+
+    // the sequence that token n belongs to: the last whose tokens start at or before it
+    int b = n, start = n, stop = n + 1;
+    if (a.q_start) {
+        b = 0;
+        for (int at = 0; at < a.c.n_seqs; at += 64) {
+            const int s = at + lane < a.c.n_seqs ? a.q_start[at + lane] : 0x7fffffff;
+            const int below = __popcll(__ballot(s <= n));
+            b += below;
+            if (below < 64) break;
+        }
+        b = b > 0 ? b - 1 : 0;
+        start = scalar_load(a.q_start, b);
+        stop = scalar_load(a.q_start, b + 1);
+        if (n < start || n >= stop) return;  // a token of no sequence
+    }
+    const int len = scalar_load(a.lens, b), j = len - (stop - n);  // its position
+    const int entry = j >> a.c.page_shift;
+    bool placed = j >= 0 && entry < a.c.max_pages;
+    int id = placed ? scalar_load(a.c.table, (int64_t)b * a.c.max_pages + entry) : -1;
+    placed = placed && (unsigned)id < (unsigned)a.c.n_pages;
+    if (!placed) {
+        id = 0;
+        report_index_error(a.c.status);
+    }
+    const int slot = j & ((1 << a.c.page_shift) - 1);
+
+    // the angles of the lane's eight pairs
+    const int pair = unit * 8;
+    const bool turns = pair * 2 < a.rot;
+    float c[8], s[8];
+    if (turns) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const int p = pair + x, axis = (p >= a.section0) + (p >= a.section01);
+            int at = a.positions ? a.positions[(int64_t)axis * a.n_tokens + n] : j;
+            if ((unsigned)at >= (unsigned)a.n_pos) {
+                report_index_error(a.c.status);
+                at = at < 0 ? 0 : a.n_pos - 1;
+            }
+            const f32x2 cs = *reinterpret_cast<const f32x2*>(a.cos_sin + ((int64_t)at * (a.rot / 2) + p) * 2);
+            c[x] = cs.x;
+            s[x] = cs.y;
+        }
+    }
+    // where a lane's 16 elements are: two runs of eight
+    const int e0 = turns && !a.interleaved ? pair : unit * 16, e1 = turns && !a.interleaved ? a.rot / 2 + pair : unit * 16 + 8;
+
+    const int step = kRows * kAppendWaves * gridDim.y;
+    for (int r0 = ((int)blockIdx.y * kAppendWaves + wave) * kRows; r0 < rows; r0 += step) {
+        const int r = r0 + sub;
+        if (r >= rows) continue;
+        const uint8_t* from;
+        uint8_t* to;
+        const bool value = r >= a.heads + G;
+        if (r < a.heads) {
+            from = a.q + (n * a.q_stride + (int64_t)r * D) * 2;
+            to = a.q_out + (n * a.q_out_stride + (int64_t)r * D) * 2;
+        } else {
+            if (!placed) continue;
+            const int h = value ? r - a.heads - G : r - a.heads;
+            from = (value ? a.v : a.k) + (n * a.kv_stride + (int64_t)h * D) * 2;
+            const int64_t place = (((int64_t)id * G + h) << a.c.page_shift) + slot;
+            to = (value ? a.c.v : a.c.k) + place * (D * 2);
+            if (value && a.weights && unit == 0) a.weights[place] = 0.f;
+        }
+        u32x4 x = *reinterpret_cast<const u32x4*>(from + e0 * 2), y = *reinterpret_cast<const u32x4*>(from + e1 * 2);
+        if (turns && !value) {
+            float f[16];
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                f[2 * w] = T::low(x[w]);
+                f[2 * w + 1] = T::high(x[w]);
+                f[8 + 2 * w] = T::low(y[w]);
+                f[8 + 2 * w + 1] = T::high(y[w]);
+            }
+            if (a.interleaved) {
+#pragma unroll
+                for (int p = 0; p < 8; ++p) turn_pair<T>(f[2 * p], f[2 * p + 1], c[p], s[p]);
+            } else {
+#pragma unroll
+                for (int p = 0; p < 8; ++p) turn_pair<T>(f[p], f[8 + p], c[p], s[p]);
+            }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                x[w] = T::pack(f[2 * w], f[2 * w + 1]);
+                y[w] = T::pack(f[8 + 2 * w], f[8 + 2 * w + 1]);
+            }
+        }
+        *reinterpret_cast<u32x4*>(to + e0 * 2) = x;
+        *reinterpret_cast<u32x4*>(to + e1 * 2) = y;
+    }
+}
+
+// ---- eviction: which positions stay
+//
+// One workgroup for a sequence's key-value head.  The largest weights are found by their bits: floats in an order-preserving
+// integer form, three passes of 11, 11 and 10 bits, each of which counts the digits of what is still undecided and keeps the
+// digit in which the last chosen one lies.  What then equals the threshold goes to the lowest positions.
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kBins = 2048;
+
+__device__ __forceinline__ uint32_t ordered(float w) {
+    if (w != w) return 0xffffffffu;  // NaN: larger than all
+    const uint32_t u = __builtin_bit_cast(uint32_t, w == 0.f ? 0.f : w);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+__global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
+    __shared__ int bins[kBins];
+    __shared__ int wave_larger[kSelectWaves], wave_equal[kSelectWaves];
+    __shared__ int found_digit, found_above;
+    const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
+    const int hk = blockIdx.x, b = blockIdx.y;
+    const int len = checked_length(a.c, a.lens, b, a.max_len);
+    int32_t* kept = a.kept + ((int64_t)b * a.c.kv_heads + hk) * a.keep;
+    if (hk == 0 && threadIdx.x == 0) a.new_lens[b] = min(len, a.keep);
+    if (len <= a.keep) {
+        for (int r = threadIdx.x; r < a.keep; r += kSelectThreads) kept[r] = r < len ? r : -1;
+        return;
+    }
+    const int others = len - a.recent;  // positions that are weighed
+    int want = a.keep - a.recent;       // of which so many stay
+    auto key = [&](int j) {
+        const int32_t id = a.c.table[(int64_t)b * a.c.max_pages + (j >> a.c.page_shift)];
+        if ((unsigned)id >= (unsigned)a.c.n_pages) {
+            report_index_error(a.c.status);
+            return 0u;
+        }
+        return ordered(a.weights[row_place(a.c, id, hk, j)]);
+    };
+    uint32_t prefix = 0, mask = 0;
+    constexpr int kShift[3] = {21, 10, 0}, kWidth[3] = {11, 11, 10};
+    if (want > 0) {
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            for (int x = threadIdx.x; x < kBins; x += kSelectThreads) bins[x] = 0;
+            __syncthreads();
+            const uint32_t digits = (1u << kWidth[pass]) - 1;
+            for (int j = threadIdx.x; j < others; j += kSelectThreads) {
+                const uint32_t u = key(j);
+                if ((u & mask) == prefix) atomicAdd(&bins[(u >> kShift[pass]) & digits], 1);
+            }
+            __syncthreads();
+            // the digit at which the counts from above reach `want`: wave 0 walks 64 bins at a time
+            if (wave == 0) {
+                int above = 0;
+                for (int top = (int)digits; top >= 0; top -= 64) {
+                    const int bin = top - lane, count = bin >= 0 ? bins[bin] : 0;
+                    int run = count;  // counts of this lane's bin and those above it in these 64
+#pragma unroll
+                    for (int d = 1; d < 64; d <<= 1) {
+                        const int other = __shfl_up(run, d);
+                        if (lane >= d) run += other;
+                    }
+                    const uint64_t reached = __ballot(above + run >= want);
+                    if (reached) {
+                        const int first = __builtin_ctzll(reached);
+                        if (lane == first) {
+                            found_digit = bin;
+                            found_above = above + run - count;
+                        }
+                        break;
+                    }
+                    above += __shfl(run, 63);
+                }
+            }
+            __syncthreads();
+            prefix |= (uint32_t)found_digit << kShift[pass];
+            mask |= digits << kShift[pass];
+            want -= found_above;  // still wanted of those with this digit
+            __syncthreads();
+        }
+    }
+    // `want` of the positions equal to the threshold stay, the lowest; all above it.  Every wave takes a run of positions: counts
+    // first, then places.
+    const bool none = a.keep == a.recent;
+    const int per_wave = (others + kSelectWaves * 64 - 1) / (kSelectWaves * 64) * 64;
+    const int j0 = wave * per_wave, j1 = min(others, j0 + per_wave);
+    int larger = 0, equal = 0;
+    for (int j = j0 + lane; j - lane < j1; j += 64) {
+        const uint32_t u = j < j1 ? key(j) : 0;
+        larger += __popcll(__ballot(j < j1 && !none && u > prefix));
+        equal += __popcll(__ballot(j < j1 && !none && u == prefix));
+    }
+    if (lane == 0) {
+        wave_larger[wave] = larger;
+        wave_equal[wave] = equal;
+    }
+    __syncthreads();
+    int place = 0, seen_equal = 0;
+    for (int w = 0; w < wave; ++w) {
+        place += wave_larger[w] + min(wave_equal[w], max(0, want - seen_equal));
+        seen_equal += wave_equal[w];
+    }
+    for (int j = j0 + lane; j - lane < j1; j += 64) {
+        const uint32_t u = j < j1 ? key(j) : 0;
+        const bool is_equal = j < j1 && !none && u == prefix;
+        const uint64_t equals = __ballot(is_equal), below = (1ull << lane) - 1;
+        const bool stays = (j < j1 && !none && u > prefix) || (is_equal && seen_equal + __popcll(equals & below) < want);
+        const uint64_t all = __ballot(stays);
+        if (stays) kept[place + __popcll(all & below)] = j;
+        place += __popcll(all);
+        seen_equal += __popcll(equals);
+    }
+    for (int r = threadIdx.x; r < a.recent; r += kSelectThreads) kept[a.keep - a.recent + r] = others + r;
+}
+
+// ---- eviction: the kept rows move
+constexpr int kMoveThreads = 256;
+
+template <int D>
+__global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
+    constexpr int kLanes = D / 8, kRows = kMoveThreads / kLanes, kEach = 4;  // lanes a row, rows at once, rows a thread
+    const int hk = blockIdx.y, b = blockIdx.z;
+    const int n = min(checked_length(a.c, a.lens, b, a.max_len), a.keep);
+    const int32_t* kept = a.kept + ((int64_t)b * a.c.kv_heads + hk) * a.keep;
+    const int part = threadIdx.x % kLanes, r0 = (int)blockIdx.x * kRows * kEach + threadIdx.x / kLanes;
+    int64_t from[kEach], to[kEach];
+    u32x4 k[kEach], v[kEach];
+    float w[kEach];
+#pragma unroll
+    for (int x = 0; x < kEach; ++x) {
+        const int r = r0 + x * kRows;
+        from[x] = to[x] = -1;
+        if (r < n) {
+            const int j = kept[r];
+            const int32_t id = a.c.table[(int64_t)b * a.c.max_pages + (j >> a.c.page_shift)];
+            const int32_t new_id = a.new_table[(int64_t)b * a.new_max_pages + (r >> a.c.page_shift)];
+            if ((unsigned)id < (unsigned)a.c.n_pages && (unsigned)new_id < (unsigned)a.c.n_pages) {
+                from[x] = row_place(a.c, id, hk, j);
+                to[x] = row_place(a.c, new_id, hk, r);
+            } else {
+                report_index_error(a.c.status);
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < kEach; ++x) {
+        if (from[x] < 0) continue;
+        k[x] = reinterpret_cast<const u32x4*>(a.c.k)[from[x] * kLanes + part];
+        v[x] = reinterpret_cast<const u32x4*>(a.c.v)[from[x] * kLanes + part];
+        w[x] = a.weights[from[x]];
+    }
+#pragma unroll
+    for (int x = 0; x < kEach; ++x) {
+        if (to[x] < 0) continue;
+        reinterpret_cast<u32x4*>(a.c.k)[to[x] * kLanes + part] = k[x];
+        reinterpret_cast<u32x4*>(a.c.v)[to[x] * kLanes + part] = v[x];
+        if (part == 0) a.weights[to[x]] = w[x];
+    }
+}
+
+template <int D>
+void launch_move(const EvictArgs& a, hipStream_t st) {
+    const int rows = kMoveThreads / (D / 8) * 4;
+    evict_move_kernel<D><<<dim3((a.keep + rows - 1) / rows, a.c.kv_heads, a.c.n_seqs), kMoveThreads, 0, st>>>(a);
+}
+
+template <class T>
+void launch_append(const AppendArgs& a, hipStream_t st) {
+    // a wave for at most 1024 / D head rows of a token where there are few tokens, all of a token's rows for four waves where
+    // they fill the chip
+    const int at_once = 1024 / a.c.dim * kAppendWaves, most = (a.heads + 2 * a.c.kv_heads + at_once - 1) / at_once;
+    const int parts = a.n_tokens >= 1024 ? 1 : most;
+    const dim3 grid(a.n_tokens, parts);
+    if (a.c.dim == 64) rope_append_kernel<T, 64><<<grid, kAppendWaves * 64, 0, st>>>(a);
+    else if (a.c.dim == 128) rope_append_kernel<T, 128><<<grid, kAppendWaves * 64, 0, st>>>(a);
+    else rope_append_kernel<T, 256><<<grid, kAppendWaves * 64, 0, st>>>(a);
+}
+
+}  // namespace
+
+int launch_rope_append(const AppendArgs& a, hipStream_t st) {
+    if (a.c.type == TMAN_TYPE_F16) launch_append<F16>(a, st);
+    else launch_append<BF16>(a, st);
+    return launch_status();
+}
+
+int launch_kv_evict(const EvictArgs& a, hipStream_t st) {
+    evict_select_kernel<<<dim3(a.c.kv_heads, a.c.n_seqs), kSelectThreads, 0, st>>>(a);
+    if (a.c.dim == 64) launch_move<64>(a, st);
+    else if (a.c.dim == 128) launch_move<128>(a, st);
+    else launch_move<256>(a, st);
+    return launch_status();
+}
+
+}  // namespace tman
