@@ -148,6 +148,14 @@ __device__ __forceinline__ float score_of(float raw, const ScoreRule& r) {
     return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap);
 }
 
+// the same less `top`, in one operation less
+template <bool CAP>
+__device__ __forceinline__ float score_from(float raw, const ScoreRule& r, float top) {
+    if constexpr (!CAP) return __builtin_fmaf(raw, r.scale, -top);
+    const float e = __builtin_amdgcn_exp2f(raw * r.scale);
+    return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap - top);
+}
+
 // Rows of keys and values in LDS.  A request (one wave, 64 x 16 bytes straight into LDS) brings 1024 bytes, whole rows; lane l's 16 bytes
 // land at 16 l of it, so an arrangement that keeps the reads off each other's banks is made by choosing which bytes a lane asks for:
 // chunk c (16 bytes) of row r is kept at place c ^ key_turn(r), or c ^ value_turn(r).

@@ -11,6 +11,8 @@
 //   * Only tiles in which some query of a wave does not see all keys compare positions.  There a hidden value may be anything,
 //     infinity and NaN included: such tiles are looked through, and what is not finite is left out of the products and added
 //     where it is seen.
+#include <type_traits>
+
 #include "tman_attn_device.h"
 
 namespace tman {
@@ -20,6 +22,7 @@ constexpr int kTile = 64;  // positions
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kTileRows = kWaves * 32;
 constexpr int kMaxSplit = 64;
+constexpr float kSlack = 8.f;
 
 // [item][piece]: every wave's accumulators as they lie in its lanes, then its maxima and sums
 __host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kTileRows * D + 2 * kTileRows; }
@@ -45,7 +48,7 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
     return ((w & e) == e ? 0xffffu : 0u) | ((w & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
 }
 
-template <class T, int D, bool CAP>
+template <class T, int D, bool CAP, bool SLOPED>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kernel(PrefillArgs a) {
     using R = RowsOf<D>;
     constexpr int kRowBytes = R::kBytes, kSlot = kTile * kRowBytes;      // of keys, and of values
@@ -127,17 +130,23 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     const u32x4* q_row = reinterpret_cast<const u32x4*>(a.q + (n * a.q_stride + (int64_t)head * D) * 2);
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) q[x] = q_row[2 * x + half];
-    const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
-    const bool sloped = a.slopes != nullptr;
-    const ScoreRule rule(a.scale, a.cap);
+    float slope = 0.f;
+    if constexpr (SLOPED) slope = a.slopes[head] * kLog2e;
+    // a scale below zero goes into the queries, so that a larger product is a larger score
+    const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) q[x] ^= flip;
+    const ScoreRule rule(fabsf(a.scale), a.cap);
 
     const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
     const uint32_t in_row = lane % (kRowBytes / 16), ask_row = lane / (kRowBytes / 16);
     const uint32_t k_ask = ask_row * kRowBytes + (in_row ^ R::key_turn(ask_row)) * 16;
     const uint32_t v_ask = ask_row * kRowBytes + (in_row ^ R::value_turn32(ask_row)) * 16;
-    auto request = [&](int t, uint32_t to) {
+    auto find = [&](int t) {
         const int j = t * kTile + wave * kOwnRows;
-        const int64_t place = row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
+        return row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
+    };
+    auto request = [&](int64_t place, uint32_t to) {
         const u32x4 k = resource(a.c.k + place, kOwnRows * kRowBytes), v = resource(a.c.v + place, kOwnRows * kRowBytes);
 #pragma unroll
         for (int i = 0; i < kRequests; ++i)
@@ -157,106 +166,135 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     for (int d = 0; d < kBlocks; ++d) out[d] = f32x16{};
     float top = kLowest, sum = 0.f;
 
-    if (t0 < t1) request(t0, all);
-    for (int t = t0; t < t1; ++t) {
-        const uint32_t buffer = all + ((t - t0) & 1) * (2 * kSlot);
-        if (t + 1 < t1) {
-            request(t + 1, all + ((t + 1 - t0) & 1) * (2 * kSlot));
-            wait_requests<2 * kRequests>();
-        } else {
-            wait_requests<0>();
-        }
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+    // one tile; PART: some query of the wave does not see all of its keys
+    auto work_on = [&](int t, uint32_t buffer, auto part) {
+        constexpr bool PART = decltype(part)::value;
         const int j0 = t * kTile;
-        if (j0 < most && j0 + kTile > least) {
-            const bool part = j0 < inner_lo || j0 + kTile > inner_hi;
-            f32x16 s[2];
+        f32x16 s[2];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                s[kb] = f32x16{};
+        for (int kb = 0; kb < 2; ++kb) {
+            s[kb] = f32x16{};
 #pragma unroll
-                for (int x = 0; x < D / 16; ++x)
-                    s[kb] = T::mfma32(lds_read<u32x4>(buffer + k_read + kb * 32 * kRowBytes + (k_chunk ^ (2 * x)) * 16), q[x], s[kb]);
-            }
-            float best = kLowest;
+            for (int x = 0; x < D / 16; ++x)
+                s[kb] = T::mfma32(lds_read<u32x4>(buffer + k_read + kb * 32 * kRowBytes + (k_chunk ^ (2 * x)) * 16), q[x], s[kb]);
+        }
+        // Where a score is a growing function of the product alone the largest product gives the largest score; otherwise the
+        // scores are made first.
+        constexpr bool kMade = PART || SLOPED;
+        float best = kMinusInf;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 16; ++i) {
+                if constexpr (kMade) {
                     const int j = j0 + 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
                     float x = score_of<CAP>(s[kb][i], rule);
-                    if (sloped) x = __builtin_fmaf(-slope, fabsf((float)(at - j)), x);
-                    if (part) x = j >= lo && j < hi ? x : kMinusInf;
+                    if constexpr (SLOPED) x = __builtin_fmaf(-slope, fabsf((float)(at - j)), x);
+                    if constexpr (PART) x = j >= lo && j < hi ? x : kMinusInf;
                     s[kb][i] = x;
-                    best = fmaxf(best, x);
                 }
-            best = fmaxf(top, max_halves(best));
-            if (__any(best > top)) {
-                const float f = __builtin_amdgcn_exp2f(top - best);
-                sum *= f;
-#pragma unroll
-                for (int d = 0; d < kBlocks; ++d) out[d] *= f;
-                top = best;
+                best = fmaxf(best, s[kb][i]);
             }
-            u32x4 p[4];  // 16 keys each
+        best = max_halves(best);
+        if constexpr (!kMade) best = score_of<CAP>(best, rule);
+        // The reference of the exponentials follows the maximum only when it has fallen behind by more than kSlack: probabilities
+        // then reach 2^kSlack, which both types hold as precisely as 1.
+        if (__any(best > top + kSlack)) {
+            const float next = fmaxf(top, best), f = __builtin_amdgcn_exp2f(top - next);
+            sum *= f;
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int d = 0; d < kBlocks; ++d) out[d] *= f;
+            top = next;
+        }
+        u32x4 p[4];  // 16 keys each
+        float more = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const float e0 = __builtin_amdgcn_exp2f(s[kb][i] - top), e1 = __builtin_amdgcn_exp2f(s[kb][i + 1] - top);
-                    sum += e0 + e1;
-                    p[2 * kb + i / 8][i % 8 / 2] = T::pack(e0, e1);
-                }
-            bool odd_values = false;
-            if (part) {
-                uint32_t odd = 0;
-                for (int x = lane; x < kSlot / 16; x += 64) {
-                    const u32x4 w = lds_read<u32x4>(buffer + kSlot + x * 16);
-                    odd |= not_finite<T>(w.x) | not_finite<T>(w.y) | not_finite<T>(w.z) | not_finite<T>(w.w);
-                }
-                odd_values = __any(odd != 0);
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                float e[2];
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    e[y] = __builtin_amdgcn_exp2f(kMade ? s[kb][i + y] - top : score_from<CAP>(s[kb][i + y], rule, top));
+                sum += e[0];
+                more += e[1];
+                p[2 * kb + i / 8][i % 8 / 2] = T::pack(e[0], e[1]);
             }
-            if (!odd_values) {
+        sum += more;
+        bool odd_values = false;
+        if constexpr (PART) {
+            uint32_t odd = 0;
+            for (int x = lane; x < kSlot / 16; x += 64) {
+                const u32x4 w = lds_read<u32x4>(buffer + kSlot + x * 16);
+                odd |= not_finite<T>(w.x) | not_finite<T>(w.y) | not_finite<T>(w.z) | not_finite<T>(w.w);
+            }
+            odd_values = __any(odd != 0);
+        }
+        if (!PART || !odd_values) {
 #pragma unroll
-                for (int ks = 0; ks < 4; ++ks)
+            for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-                    for (int d = 0; d < kBlocks; ++d) {
-                        const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
-                        const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
-                        out[d] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p[ks], out[d]);
-                    }
-            } else {
-                for (int ks = 0; ks < 4; ++ks) {
-                    const u32x4 pk = ks == 0 ? p[0] : ks == 1 ? p[1] : ks == 2 ? p[2] : p[3];
-#pragma unroll
-                    for (int d = 0; d < kBlocks; ++d) {
-                        const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
-                        const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
-                        out[d] = T::mfma32(u32x4{v0.x & ~not_finite<T>(v0.x), v0.y & ~not_finite<T>(v0.y), v1.x & ~not_finite<T>(v1.x),
-                                                 v1.y & ~not_finite<T>(v1.y)}, pk, out[d]);
-                    }
+                for (int d = 0; d < kBlocks; ++d) {
+                    const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
+                    const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
+                    out[d] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p[ks], out[d]);
                 }
-                for (int y = 0; y < kTile; ++y) {
-                    const bool seen = j0 + y >= lo && j0 + y < hi;
+        } else {
+            for (int ks = 0; ks < 4; ++ks) {
+                const u32x4 pk = ks == 0 ? p[0] : ks == 1 ? p[1] : ks == 2 ? p[2] : p[3];
 #pragma unroll
-                    for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t place = (4 * d + i) ^ R::value_turn32(y);
-                            const u32x2 w = lds_read<u32x2>(buffer + kSlot + y * kRowBytes + place * 16 + half * 8);
-                            const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
-                            if (seen && (m.x & 0xffffu)) out[d][4 * i] += T::low(w.x);
-                            if (seen && (m.x >> 16)) out[d][4 * i + 1] += T::high(w.x);
-                            if (seen && (m.y & 0xffffu)) out[d][4 * i + 2] += T::low(w.y);
-                            if (seen && (m.y >> 16)) out[d][4 * i + 3] += T::high(w.y);
-                        }
+                for (int d = 0; d < kBlocks; ++d) {
+                    const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
+                    const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
+                    out[d] = T::mfma32(u32x4{v0.x & ~not_finite<T>(v0.x), v0.y & ~not_finite<T>(v0.y), v1.x & ~not_finite<T>(v1.x),
+                                             v1.y & ~not_finite<T>(v1.y)}, pk, out[d]);
                 }
+            }
+            for (int y = 0; y < kTile; ++y) {
+                const bool seen = j0 + y >= lo && j0 + y < hi;
+#pragma unroll
+                for (int d = 0; d < kBlocks; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t place = (4 * d + i) ^ R::value_turn32(y);
+                        const u32x2 w = lds_read<u32x2>(buffer + kSlot + y * kRowBytes + place * 16 + half * 8);
+                        const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
+                        if (seen && (m.x & 0xffffu)) out[d][4 * i] += T::low(w.x);
+                        if (seen && (m.x >> 16)) out[d][4 * i + 1] += T::high(w.x);
+                        if (seen && (m.y & 0xffffu)) out[d][4 * i + 2] += T::low(w.y);
+                        if (seen && (m.y >> 16)) out[d][4 * i + 3] += T::high(w.y);
+                    }
             }
         }
+    };
+
+    int64_t next = 0;
+    if (t0 < t1) {
+        request(find(t0), all);
+        if (t0 + 1 < t1) next = find(t0 + 1);
+    }
+    auto enter = [&](int t) {  // tile t is there, its buffer's neighbour is free and takes the next one
+        wait_requests<0>();
         wait_lds();
-        __builtin_amdgcn_s_barrier();  // all have read this buffer
+        __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        if (t + 1 < t1) {
+            request(next, all + ((t + 1 - t0) & 1) * (2 * kSlot));
+            if (t + 2 < t1) next = find(t + 2);
+        }
+        return all + ((t - t0) & 1) * (2 * kSlot);
+    };
+    // The tiles that all queries of the wave see whole are a run; before and behind it, positions are compared.  Waves pass the
+    // same number of barriers, whichever loop they are in.
+    const int whole0 = min(max((inner_lo + kTile - 1) / kTile, t0), t1), whole1 = min(max(inner_hi / kTile, whole0), t1);
+    int t = t0, stop = whole0;
+    while (t < t1) {
+        for (; t < stop; ++t) {
+            const uint32_t buffer = enter(t);
+            if (t * kTile < most && (t + 1) * kTile > least) work_on(t, buffer, std::true_type{});
+        }
+        for (; t < whole1; ++t) work_on(t, enter(t), std::false_type{});
+        stop = t1;
     }
     sum = sum_halves(sum);
 
@@ -319,7 +357,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
 
 template <class T, int D>
 void launch_of(const PrefillArgs& a, int grid, hipStream_t st) {
-    auto* kernel = a.cap > 0.f ? attn_prefill_kernel<T, D, true> : attn_prefill_kernel<T, D, false>;
+    const bool cap = a.cap > 0.f, sloped = a.slopes != nullptr;
+    auto* kernel = cap ? (sloped ? attn_prefill_kernel<T, D, true, true> : attn_prefill_kernel<T, D, true, false>)
+                       : (sloped ? attn_prefill_kernel<T, D, false, true> : attn_prefill_kernel<T, D, false, false>);
     kernel<<<grid, kThreads, 0, st>>>(a);
 }
 
