@@ -23,6 +23,7 @@ constexpr size_t kAttnTicketBytes = kAttnTickets * sizeof(int32_t);
 struct DecodePlan {
     int head_chunks;   // of 16 query heads a key-value head
     int n_split;       // pieces, at most
+    int n_slots;       // of partial sums: the pieces and the groups that they meet in first where they are many
     int split_tiles;   // tiles of 32 positions in a piece
     int score_stride;  // floats from one head's scores to the next's (accumulated weights only)
     size_t partial_at, score_at, lse_at, bytes;

@@ -20,6 +20,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kHeads = 16;  // query heads of a workgroup, at most
 constexpr int kMaxSplit = 256;
+constexpr int kAtOnce = 8;  // pieces that a thread of the join reads at once
+constexpr int kGroup = 32;  // pieces that meet at once
 
 // [row item][piece]: heads x D sums, then the maxima and the sums of probabilities
 __host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kHeads * D + 2 * kHeads; }
@@ -206,8 +208,23 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
     __syncthreads();
 
     const int64_t item = ((int64_t)b * a.c.kv_heads + hk) * a.p.head_chunks + chunk;
-    float* partial = a.partial + (item * a.p.n_split + blockIdx.x) * partial_floats(D);
+    float* partial = a.partial + (item * a.p.n_slots + blockIdx.x) * partial_floats(D);
     const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
+    auto finish = [&](int h, int d, float m, float l, f32x4 o) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        *reinterpret_cast<u32x2*>(a.out + (b * a.out_stride + (int64_t)(h0 + h) * D + d) * 2) =
+            u32x2{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+        if (d == 0) {
+            const float l2 = m + __builtin_amdgcn_logf(l);
+            if (a.lse) a.lse[(int64_t)b * a.heads + h0 + h] = l == 0.f ? kMinusInf : l2 * kLn2;
+            if constexpr (WEIGHTS) a.lse2[(int64_t)b * a.heads + h0 + h] = l == 0.f ? kMinusInf : l2;
+        }
+    };
+    auto publish = [&](float* to, int h, int d, float m, float l, f32x4 o) {
+        store_shared(to + h * D + d, o[0], o[1]);
+        store_shared(to + h * D + d + 2, o[2], o[3]);
+        if (d == 0) store_shared(to + kHeads * D + 2 * h, m, l);
+    };
     for (int x = threadIdx.x; x < n_heads * (D / 4); x += kThreads) {
         const int h = x / (D / 4), d = x % (D / 4) * 4;
         float m = wave_max[0][h];
@@ -222,70 +239,94 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
             o += f * lds_read<f32x4>(all + w * kWaveBytes + (h * kOut + d) * 4);
         }
         if (pieces == 1) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            *reinterpret_cast<u32x2*>(a.out + (b * a.out_stride + (int64_t)(h0 + h) * D + d) * 2) =
-                u32x2{T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
-            if (d == 0) {
-                const float l2 = m + __builtin_amdgcn_logf(l);
-                if (a.lse) a.lse[(int64_t)b * a.heads + h0 + h] = l == 0.f ? kMinusInf : l2 * kLn2;
-                if constexpr (WEIGHTS) a.lse2[(int64_t)b * a.heads + h0 + h] = l == 0.f ? kMinusInf : l2;
-            }
+            finish(h, d, m, l, o);
         } else {
-            store_shared(partial + h * D + d, o[0], o[1]);
-            store_shared(partial + h * D + d + 2, o[2], o[3]);
-            if (d == 0) store_shared(partial + kHeads * D + 2 * h, m, l);
+            publish(partial, h, d, m, l, o);
         }
     }
     if (pieces == 1) return;
 
-    // the last piece to arrive adds them all up, in the order of the pieces
-    wait_requests<0>();  // this piece's sums have reached device-coherent memory
-    __syncthreads();
-    if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.tickets + item, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
-    __syncthreads();
-    if (!last) return;
-    const float* base = a.partial + item * a.p.n_split * partial_floats(D);
-    // factors of the pieces: [piece][head] in LDS, and per head the maximum and the sum
-    lds_pointer<float> factor = (lds_pointer<float>)room;
-    for (int x = threadIdx.x; x < pieces * n_heads; x += kThreads) {
-        const int p = x / n_heads, h = x - p * n_heads;
-        const f32x2 ml = load_shared(base + p * partial_floats(D) + kHeads * D + 2 * h);
-        factor[p * 2 * kHeads + h] = ml.x;
-        factor[p * 2 * kHeads + kHeads + h] = ml.y;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < n_heads) {
-        const int h = threadIdx.x;
-        float m = kLowest, l = 0.f;
-        for (int p = 0; p < pieces; ++p) m = fmaxf(m, factor[p * 2 * kHeads + h]);
-        for (int p = 0; p < pieces; ++p) {
-            const float f = __builtin_amdgcn_exp2f(factor[p * 2 * kHeads + h] - m);
-            factor[p * 2 * kHeads + h] = f;
-            l = __builtin_fmaf(f, factor[p * 2 * kHeads + kHeads + h], l);
+    // The last piece to arrive adds them up, in the order of the pieces; many pieces meet in groups first, whose last ones meet.
+    // A thread takes four coordinates of a head and every kShares-th piece, with the reads of several pieces under way at once; the
+    // shares then meet in LDS.
+    float* base = a.partial + item * a.p.n_slots * partial_floats(D);
+    const int quads = n_heads * (D / 4);
+    auto arrive = [&](int32_t* ticket, int of) {  // whether this workgroup is the last; its sums have reached coherent memory
+        wait_requests<0>();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
+            if (last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        wave_max[0][h] = m;
-        wave_sum[0][h] = l;
-    }
-    __syncthreads();
-    for (int x = threadIdx.x; x < n_heads * (D / 2); x += kThreads) {
-        const int h = x / (D / 2), d = x % (D / 2) * 2;
-        f32x2 o = {0, 0};
-#pragma unroll 8
-        for (int p = 0; p < pieces; ++p) {
-            const float f = factor[p * 2 * kHeads + h];
-            const f32x2 v = load_shared(base + p * partial_floats(D) + h * D + d);
-            o.x = __builtin_fmaf(f, v.x, o.x);
-            o.y = __builtin_fmaf(f, v.y, o.y);
+        __syncthreads();
+        return last != 0;
+    };
+    auto join = [&](int first, int count, auto done) {
+        int shares = 1;
+        while (shares * 2 * quads <= kThreads && shares * kAtOnce < count) shares *= 2;
+        for (int x = threadIdx.x; x < quads * shares; x += kThreads) {
+            const int share = x / quads, y = x - share * quads, h = y / (D / 4), d = y % (D / 4) * 4;
+            float m = kLowest, l = 0.f;
+            f32x4 o = {0, 0, 0, 0};
+            for (int p0 = share; p0 < count; p0 += kAtOnce * shares) {
+                f32x2 ml[kAtOnce], v[kAtOnce][2];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const float* from = base + (first + min(p0 + k * shares, count - 1)) * partial_floats(D);
+                    ml[k] = load_shared(from + kHeads * D + 2 * h);
+                    v[k][0] = load_shared(from + h * D + d);
+                    v[k][1] = load_shared(from + h * D + d + 2);
+                }
+                float next = m;
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
+                const float f = __builtin_amdgcn_exp2f(m - next);
+                l *= f;
+                o *= f;
+                m = next;
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (p0 + k * shares >= count) continue;
+                    const float e = __builtin_amdgcn_exp2f(ml[k].x - m);
+                    l = __builtin_fmaf(e, ml[k].y, l);
+                    o += e * f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y};
+                }
+            }
+            if (shares > 1) {
+                lds_write(all + x * 16, o);
+                lds_write(all + kThreads * 16 + x * 8, f32x2{m, l});
+            } else {
+                done(h, d, m, l, o);
+            }
         }
-        const float m = wave_max[0][h], l = wave_sum[0][h], inv = l == 0.f ? 0.f : 1.f / l;
-        *reinterpret_cast<uint32_t*>(a.out + (b * a.out_stride + (int64_t)(h0 + h) * D + d) * 2) = T::pack(o.x * inv, o.y * inv);
-        if (d == 0) {
-            const float l2 = m + __builtin_amdgcn_logf(l);
-            if (a.lse) a.lse[(int64_t)b * a.heads + h0 + h] = l == 0.f ? kMinusInf : l2 * kLn2;
-            if constexpr (WEIGHTS) a.lse2[(int64_t)b * a.heads + h0 + h] = l == 0.f ? kMinusInf : l2;
+        if (shares == 1) return;
+        __syncthreads();
+        for (int y = threadIdx.x; y < quads; y += kThreads) {
+            const int h = y / (D / 4), d = y % (D / 4) * 4;
+            float m = kLowest, l = 0.f;
+            f32x4 o = {0, 0, 0, 0};
+            for (int s = 0; s < shares; ++s) m = fmaxf(m, lds_read<f32x2>(all + kThreads * 16 + (s * quads + y) * 8).x);
+            for (int s = 0; s < shares; ++s) {
+                const f32x2 ml = lds_read<f32x2>(all + kThreads * 16 + (s * quads + y) * 8);
+                const float e = __builtin_amdgcn_exp2f(ml.x - m);
+                l = __builtin_fmaf(e, ml.y, l);
+                o += e * lds_read<f32x4>(all + (s * quads + y) * 16);
+            }
+            done(h, d, m, l, o);
         }
+    };
+    int32_t* tickets = a.tickets + item * (1 + a.p.n_slots - a.p.n_split);
+    if (pieces <= kGroup) {
+        if (arrive(tickets, pieces)) join(0, pieces, finish);
+        return;
     }
-    if (threadIdx.x == 0) __hip_atomic_store(a.tickets + item, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int group = (int)blockIdx.x / kGroup, groups = (pieces + kGroup - 1) / kGroup;
+    const int members = min(kGroup, pieces - group * kGroup);
+    if (!arrive(tickets + 1 + group, members)) return;
+    join(group * kGroup, members, [&](int h, int d, float m, float l, f32x4 o) {
+        publish(base + (a.p.n_split + group) * partial_floats(D), h, d, m, l, o);
+    });
+    if (arrive(tickets, groups)) join(a.p.n_split, groups, finish);
 }
 
 // Accumulated weights: once a row's sum is known, its probabilities come out of the kept scores; a thread adds those of the heads of
@@ -300,12 +341,22 @@ __global__ __launch_bounds__(kWeightThreads) void attn_weights_kernel(DecodeArgs
     if (j >= len) return;
     const int64_t h0 = (int64_t)b * a.heads + hk * a.group;
     f32x4 add = {0, 0, 0, 0};
-    for (int h = 0; h < a.group; ++h) {
-        const float l2 = a.lse2[h0 + h];
-        if (l2 == kMinusInf) continue;
-        const f32x4 s = *reinterpret_cast<const f32x4*>(a.scores + (h0 + h) * a.p.score_stride + j);
+    constexpr int kHeadsAtOnce = 8;
+    for (int g0 = 0; g0 < a.group; g0 += kHeadsAtOnce) {
+        float l2[kHeadsAtOnce];
+        f32x4 s[kHeadsAtOnce];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) add[r] += __builtin_amdgcn_exp2f(s[r] - l2);
+        for (int g = 0; g < kHeadsAtOnce; ++g) {
+            const int64_t h = h0 + min(g0 + g, a.group - 1);
+            l2[g] = a.lse2[h];
+            s[g] = *reinterpret_cast<const f32x4*>(a.scores + h * a.p.score_stride + j);
+        }
+#pragma unroll
+        for (int g = 0; g < kHeadsAtOnce; ++g) {
+            if (g0 + g >= a.group || l2[g] == kMinusInf) continue;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) add[r] += __builtin_amdgcn_exp2f(s[g][r] - l2[g]);
+        }
     }
     const int e = min(j >> a.c.page_shift, a.c.max_pages - 1);
     const int id = a.c.table[(int64_t)b * a.c.max_pages + e];
@@ -333,7 +384,7 @@ int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // A launch wants enough pieces to fill the chip and to even out sequences of different lengths, and no more than that, since pieces
 // meet through memory.
-constexpr int kWantedWorkgroups = 1024;
+constexpr int kWantedWorkgroups = 256;
 constexpr int kLeastTiles = 4;  // of a piece: one for each wave
 
 DecodePlan plan_attn_decode(const tman_kv_cache_t* c, const tman_attn_t* a, int max_len, bool weights) {
@@ -349,9 +400,10 @@ DecodePlan plan_attn_decode(const tman_kv_cache_t* c, const tman_attn_t* a, int 
     if (pieces < 1) pieces = 1;
     p.split_tiles = ceil_div(tiles, pieces);
     p.n_split = pieces;  // (as many as room is kept for: a longer max_len never needs less)
+    p.n_slots = pieces + (pieces > kGroup ? ceil_div(pieces, kGroup) : 0);
     p.score_stride = ceil_div(max_len, kTile) * kTile;
     p.partial_at = kAttnTicketBytes;
-    p.score_at = p.partial_at + (pieces > 1 ? rows * pieces * partial_floats(c->dim) * sizeof(float) : 0);
+    p.score_at = p.partial_at + (pieces > 1 ? rows * p.n_slots * partial_floats(c->dim) * sizeof(float) : 0);
     p.lse_at = p.score_at + (weights ? (size_t)c->n_seqs * a->heads * p.score_stride * sizeof(float) : 0);
     p.bytes = p.lse_at + (weights ? (size_t)c->n_seqs * a->heads * sizeof(float) : 0);
     return p;

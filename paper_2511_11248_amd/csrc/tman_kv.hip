@@ -123,8 +123,11 @@ __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendAr
 // ---- eviction: which positions stay
 //
 // One workgroup for a sequence's key-value head.  The largest weights are found by their bits: floats in an order-preserving
-// integer form, three passes of 11, 11 and 10 bits, each of which counts the digits of what is still undecided and keeps the
-// digit in which the last chosen one lies.  What then equals the threshold goes to the lowest positions.
+// integer form, up to three passes of 11, 11 and 10 bits, each of which counts the digits of what is still undecided and keeps the
+// digit in which the last chosen one lies; it ends early where all with that digit are chosen.  What then equals the threshold
+// goes to the lowest positions.
+// What bounds it: one unit's latency, so everything is read four positions at a time with several reads under way, and kept in LDS
+// where it fits (CACHE positions).
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
 
@@ -134,10 +137,22 @@ __device__ __forceinline__ uint32_t ordered(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Inclusive sum over the lanes up to this one.
+__device__ __forceinline__ int sum_up_to(int x, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int other = __shfl_up(x, d);
+        if (lane >= d) x += other;
+    }
+    return x;
+}
+
+template <int CACHE>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
+    __shared__ __attribute__((aligned(16))) uint32_t cache[CACHE ? CACHE : 4];
     __shared__ int bins[kBins];
     __shared__ int wave_larger[kSelectWaves], wave_equal[kSelectWaves];
-    __shared__ int found_digit, found_above;
+    __shared__ int found_digit, found_above, found_count;
     const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
     const int hk = blockIdx.x, b = blockIdx.y;
     const int len = checked_length(a.c, a.lens, b, a.max_len);
@@ -149,68 +164,90 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     }
     const int others = len - a.recent;  // positions that are weighed
     int want = a.keep - a.recent;       // of which so many stay
-    auto key = [&](int j) {
-        const int32_t id = a.c.table[(int64_t)b * a.c.max_pages + (j >> a.c.page_shift)];
-        if ((unsigned)id >= (unsigned)a.c.n_pages) {
-            report_index_error(a.c.status);
-            return 0u;
-        }
-        return ordered(a.weights[row_place(a.c, id, hk, j)]);
-    };
-    uint32_t prefix = 0, mask = 0;
-    constexpr int kShift[3] = {21, 10, 0}, kWidth[3] = {11, 11, 10};
-    if (want > 0) {
+    for (int r = threadIdx.x; r < a.recent; r += kSelectThreads) kept[want + r] = others + r;
+    if (want == 0) return;
+    const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
+
+    // calls f(j, keys of positions j to j + 3) for j = start, start + step, ... below stop, by all lanes of a wave together
+    auto from_memory = [&](int start, int step, int stop, auto f) {
+        constexpr int kAhead = 4;
+        for (int j = start; j - lane * 4 < stop; j += kAhead * step) {
+            int id[kAhead];
+            f32x4 w[kAhead];
 #pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            for (int x = threadIdx.x; x < kBins; x += kSelectThreads) bins[x] = 0;
-            __syncthreads();
-            const uint32_t digits = (1u << kWidth[pass]) - 1;
-            for (int j = threadIdx.x; j < others; j += kSelectThreads) {
-                const uint32_t u = key(j);
-                if ((u & mask) == prefix) atomicAdd(&bins[(u >> kShift[pass]) & digits], 1);
-            }
-            __syncthreads();
-            // the digit at which the counts from above reach `want`: wave 0 walks 64 bins at a time
-            if (wave == 0) {
-                int above = 0;
-                for (int top = (int)digits; top >= 0; top -= 64) {
-                    const int bin = top - lane, count = bin >= 0 ? bins[bin] : 0;
-                    int run = count;  // counts of this lane's bin and those above it in these 64
+            for (int x = 0; x < kAhead; ++x) id[x] = j + x * step < stop ? table[(j + x * step) >> a.c.page_shift] : 0;
 #pragma unroll
-                    for (int d = 1; d < 64; d <<= 1) {
-                        const int other = __shfl_up(run, d);
-                        if (lane >= d) run += other;
-                    }
-                    const uint64_t reached = __ballot(above + run >= want);
-                    if (reached) {
-                        const int first = __builtin_ctzll(reached);
-                        if (lane == first) {
-                            found_digit = bin;
-                            found_above = above + run - count;
-                        }
-                        break;
-                    }
-                    above += __shfl(run, 63);
+            for (int x = 0; x < kAhead; ++x) {
+                w[x] = f32x4{0, 0, 0, 0};
+                if (j + x * step < stop) {
+                    if ((unsigned)id[x] < (unsigned)a.c.n_pages)
+                        w[x] = *reinterpret_cast<const f32x4*>(a.weights + row_place(a.c, id[x], hk, j + x * step));
+                    else
+                        report_index_error(a.c.status);
                 }
             }
-            __syncthreads();
-            prefix |= (uint32_t)found_digit << kShift[pass];
-            mask |= digits << kShift[pass];
-            want -= found_above;  // still wanted of those with this digit
-            __syncthreads();
+#pragma unroll
+            for (int x = 0; x < kAhead; ++x)
+                if (j + x * step - lane * 4 < stop) f(j + x * step, u32x4{ordered(w[x].x), ordered(w[x].y), ordered(w[x].z), ordered(w[x].w)});
         }
+    };
+    auto each = [&](int start, int step, int stop, auto f) {
+        if constexpr (CACHE > 0) {
+            for (int j = start; j - lane * 4 < stop; j += step) f(j, *reinterpret_cast<const u32x4*>(cache + min(j, CACHE - 4)));
+        } else {
+            from_memory(start, step, stop, f);
+        }
+    };
+    if constexpr (CACHE > 0)
+        from_memory((int)threadIdx.x * 4, kSelectThreads * 4, others, [&](int j, u32x4 u) {
+            if (j < others) *reinterpret_cast<u32x4*>(cache + j) = u;
+        });
+
+    uint32_t prefix = 0, mask = 0;
+    constexpr int kShift[3] = {21, 10, 0}, kWidth[3] = {11, 11, 10};
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+        for (int x = threadIdx.x; x < kBins; x += kSelectThreads) bins[x] = 0;
+        __syncthreads();
+        const uint32_t digits = (1u << kWidth[pass]) - 1;
+        each((int)threadIdx.x * 4, kSelectThreads * 4, others, [&](int j, u32x4 u) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (j + r < others && (u[r] & mask) == prefix) atomicAdd(&bins[(u[r] >> kShift[pass]) & digits], 1);
+        });
+        __syncthreads();
+        // counts from the highest digit down, two digits a thread: where do they reach `want`?
+        const int high = kBins - 1 - 2 * (int)threadIdx.x, c0 = bins[high], c1 = bins[high - 1];
+        int run = sum_up_to(c0 + c1, lane);
+        if (lane == 63) wave_larger[wave] = run;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) run += wave_larger[w];
+        const int above = run - c0 - c1;
+        if (above < want && want <= run) {
+            const bool first = want <= above + c0;
+            found_digit = first ? high : high - 1;
+            found_above = first ? above : above + c0;
+            found_count = first ? c0 : c1;
+        }
+        __syncthreads();
+        prefix |= (uint32_t)found_digit << kShift[pass];
+        mask |= digits << kShift[pass];
+        want -= found_above;  // still wanted of those with this digit
+        if (want == found_count) break;
     }
-    // `want` of the positions equal to the threshold stay, the lowest; all above it.  Every wave takes a run of positions: counts
-    // first, then places.
-    const bool none = a.keep == a.recent;
-    const int per_wave = (others + kSelectWaves * 64 - 1) / (kSelectWaves * 64) * 64;
+    __syncthreads();
+    // all above the threshold stay, and the lowest `want` positions of those equal to it.  Every wave takes a run of positions:
+    // counts first, then places.
+    const int per_wave = (others + kSelectWaves * 256 - 1) / (kSelectWaves * 256) * 256;
     const int j0 = wave * per_wave, j1 = min(others, j0 + per_wave);
     int larger = 0, equal = 0;
-    for (int j = j0 + lane; j - lane < j1; j += 64) {
-        const uint32_t u = j < j1 ? key(j) : 0;
-        larger += __popcll(__ballot(j < j1 && !none && u > prefix));
-        equal += __popcll(__ballot(j < j1 && !none && u == prefix));
-    }
+    each(j0 + lane * 4, 256, j1, [&](int j, u32x4 u) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            larger += __popcll(__ballot(j + r < j1 && (u[r] & mask) > prefix));
+            equal += __popcll(__ballot(j + r < j1 && (u[r] & mask) == prefix));
+        }
+    });
     if (lane == 0) {
         wave_larger[wave] = larger;
         wave_equal[wave] = equal;
@@ -221,17 +258,32 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
         place += wave_larger[w] + min(wave_equal[w], max(0, want - seen_equal));
         seen_equal += wave_equal[w];
     }
-    for (int j = j0 + lane; j - lane < j1; j += 64) {
-        const uint32_t u = j < j1 ? key(j) : 0;
-        const bool is_equal = j < j1 && !none && u == prefix;
-        const uint64_t equals = __ballot(is_equal), below = (1ull << lane) - 1;
-        const bool stays = (j < j1 && !none && u > prefix) || (is_equal && seen_equal + __popcll(equals & below) < want);
-        const uint64_t all = __ballot(stays);
-        if (stays) kept[place + __popcll(all & below)] = j;
-        place += __popcll(all);
-        seen_equal += __popcll(equals);
-    }
-    for (int r = threadIdx.x; r < a.recent; r += kSelectThreads) kept[a.keep - a.recent + r] = others + r;
+    const uint64_t below = (1ull << lane) - 1;
+    each(j0 + lane * 4, 256, j1, [&](int j, u32x4 u) {
+        bool is_equal[4], stays[4];
+        int before = seen_equal, total = 0;  // equal ones at lower positions, and of all lanes
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            is_equal[r] = j + r < j1 && (u[r] & mask) == prefix;
+            const uint64_t m = __ballot(is_equal[r]);
+            before += __popcll(m & below);
+            total += __popcll(m);
+        }
+        int at = place, kept_here = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            stays[r] = (j + r < j1 && (u[r] & mask) > prefix) || (is_equal[r] && before < want);
+            before += is_equal[r];
+            const uint64_t m = __ballot(stays[r]);
+            at += __popcll(m & below);
+            kept_here += __popcll(m);
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (stays[r]) kept[at++] = j + r;
+        place += kept_here;
+        seen_equal += total;
+    });
 }
 
 // ---- eviction: the kept rows move
@@ -306,7 +358,11 @@ int launch_rope_append(const AppendArgs& a, hipStream_t st) {
 }
 
 int launch_kv_evict(const EvictArgs& a, hipStream_t st) {
-    evict_select_kernel<<<dim3(a.c.kv_heads, a.c.n_seqs), kSelectThreads, 0, st>>>(a);
+    // what is weighed is kept in LDS where that holds it; the small form leaves room for two workgroups a unit
+    const dim3 grid(a.c.kv_heads, a.c.n_seqs);
+    if (a.max_len <= 8192) evict_select_kernel<8192><<<grid, kSelectThreads, 0, st>>>(a);
+    else if (a.max_len <= 32768) evict_select_kernel<32768><<<grid, kSelectThreads, 0, st>>>(a);
+    else evict_select_kernel<0><<<grid, kSelectThreads, 0, st>>>(a);
     if (a.c.dim == 64) launch_move<64>(a, st);
     else if (a.c.dim == 128) launch_move<128>(a, st);
     else launch_move<256>(a, st);
