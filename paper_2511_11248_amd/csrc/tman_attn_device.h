@@ -9,6 +9,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
@@ -136,9 +137,13 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 
 // Scores are made in units of log2: exp2 needs no product then.  raw = q . k.
 struct ScoreRule {
-    float scale;    // scale * log2 e, capped: 2 scale log2 e / cap
-    float cap;      // cap * log2 e, or 0
-    __device__ __forceinline__ ScoreRule(float s, float c) : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e) {}
+    float scale;       // scale * log2 e, capped: 2 scale log2 e / cap
+    float cap;         // cap * log2 e, or 0
+    float linear;      // capped: scale / cap
+    float p[5];        // capped: cap * log2 e times the coefficients of tanh(x) / x in x^2
+    __device__ __forceinline__ ScoreRule(float s, float c)
+        : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e), linear(c > 0.f ? s / c : 0.f),
+          p{cap * 0.99999993f, cap * -0.33332302f, cap * 0.13310064f, cap * -0.05209665f, cap * 0.01546875f} {}
 };
 // cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of 2^-23 cap, whatever x.
 template <bool CAP>
@@ -147,13 +152,23 @@ __device__ __forceinline__ float score_of(float raw, const ScoreRule& r) {
     const float e = __builtin_amdgcn_exp2f(raw * r.scale);
     return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap);
 }
-
 // the same less `top`, in one operation less
 template <bool CAP>
 __device__ __forceinline__ float score_from(float raw, const ScoreRule& r, float top) {
     if constexpr (!CAP) return __builtin_fmaf(raw, r.scale, -top);
     const float e = __builtin_amdgcn_exp2f(raw * r.scale);
     return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap - top);
+}
+// ... and without the exponential and the reciprocal, each of which takes the time of four products: for |x| up to
+// kSmallTanh an interpolation at the Chebyshev points, off by 8e-8 of the result at most.
+constexpr float kSmallTanh = 0.6f;
+__device__ __forceinline__ float small_score_from(float raw, const ScoreRule& r, float top) {
+    const float x = raw * r.linear, u = x * x;
+    float f = __builtin_fmaf(u, r.p[4], r.p[3]);
+    f = __builtin_fmaf(u, f, r.p[2]);
+    f = __builtin_fmaf(u, f, r.p[1]);
+    f = __builtin_fmaf(u, f, r.p[0]);
+    return __builtin_fmaf(x, f, -top);
 }
 
 // Rows of keys and values in LDS.  A request (one wave, 64 x 16 bytes straight into LDS) brings 1024 bytes, whole rows; lane l's 16 bytes

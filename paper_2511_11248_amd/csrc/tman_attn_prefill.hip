@@ -18,11 +18,13 @@
 namespace tman {
 namespace {
 
-constexpr int kTile = 64;  // positions
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kTileRows = kWaves * 32;
 constexpr int kMaxSplit = 64;
 constexpr float kSlack = 8.f;
+
+// Positions of a tile: heads of 256 leave registers for the scores of 32.
+__host__ __device__ constexpr int tile_of(int D) { return D == 256 ? 32 : 64; }
 
 // [item][piece]: every wave's accumulators as they lie in its lanes, then its maxima and sums
 __host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kTileRows * D + 2 * kTileRows; }
@@ -51,8 +53,9 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
 template <class T, int D, bool CAP, bool SLOPED>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kernel(PrefillArgs a) {
     using R = RowsOf<D>;
+    constexpr int kTile = tile_of(D), kKeyBlocks = kTile / 32;          // positions
     constexpr int kRowBytes = R::kBytes, kSlot = kTile * kRowBytes;      // of keys, and of values
-    constexpr int kOwnRows = kTile / kWaves;                            // rows that a wave requests of a tile: 16, in one page
+    constexpr int kOwnRows = kTile / kWaves;                            // rows that a wave requests of a tile: 8 or 16, in one page
     constexpr int kRequests = kOwnRows * kRowBytes / 1024;              // and as many requests for the values
     constexpr int kBlocks = D / 32;
     __shared__ __attribute__((aligned(1024))) uint8_t room[2 * 2 * kSlot];
@@ -108,6 +111,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     // of the wave: everything that is seen lies in [least, most), what all see in [inner_lo, inner_hi)
     const int least = min_of_columns(sees ? lo : 0x7fffffff), most = -min_of_columns(sees ? -hi : 0);
     const int inner_lo = -min_of_columns(sees ? -lo : 0), inner_hi = min_of_columns(sees ? hi : 0x7fffffff);
+    const int least_at = min_of_columns(sees ? at : 0x7fffffff);
     if (lane == 0) {
         wave_lo[wave] = least;
         wave_hi[wave] = most;
@@ -140,8 +144,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
 
     const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
     const uint32_t in_row = lane % (kRowBytes / 16), ask_row = lane / (kRowBytes / 16);
-    const uint32_t k_ask = ask_row * kRowBytes + (in_row ^ R::key_turn(ask_row)) * 16;
-    const uint32_t v_ask = ask_row * kRowBytes + (in_row ^ R::value_turn32(ask_row)) * 16;
+    const uint32_t k_ask = ask_row * kRowBytes + (in_row ^ R::key_turn(wave * kOwnRows + ask_row)) * 16;
+    const uint32_t v_ask = ask_row * kRowBytes + (in_row ^ R::value_turn32(wave * kOwnRows + ask_row)) * 16;
     auto find = [&](int t) {
         const int j = t * kTile + wave * kOwnRows;
         return row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
@@ -156,47 +160,87 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             request_to_lds(v, v_ask ^ (R::value_turn32(i * R::kRowsPerRequest) * 16), i * 1024, to + kSlot + (wave * kRequests + i) * 1024);
     };
     // reads: keys of row 32 kb + col, chunk 2 x + half; values of rows .. + 4 half, columns 32 d + 16 (lane / 16 % 2) ..
-    const uint32_t k_read = col * kRowBytes, k_chunk = half ^ R::key_turn(col);
+    // (turns reach the lowest 256 bytes of a row: what is further is a constant)
+    constexpr int kKeyReads = D / 16 < 8 ? D / 16 : 8, kValueReads = kBlocks < 4 ? kBlocks : 4;
+    uint32_t k_read[kKeyReads], v_read[kValueReads];
+#pragma unroll
+    for (int x = 0; x < kKeyReads; ++x) k_read[x] = all + col * kRowBytes + ((half ^ R::key_turn(col)) ^ (2 * x)) * 16;
     const int v_row = 4 * half + ((lane & 15) >> 2);
-    const uint32_t v_read = kSlot + v_row * kRowBytes + (lane & 1) * 8;
-    const uint32_t v_chunk = (((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) ^ R::value_turn32(v_row);
+#pragma unroll
+    for (int d = 0; d < kValueReads; ++d)
+        v_read[d] = all + kSlot + v_row * kRowBytes + (lane & 1) * 8 +
+                    ((((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) ^ R::value_turn32(v_row) ^ (4 * d)) * 16;
+    // kept, not made again for every tile
+#pragma unroll
+    for (int x = 0; x < kKeyReads; ++x) asm volatile("" : "+v"(k_read[x]));
+#pragma unroll
+    for (int d = 0; d < kValueReads; ++d) asm volatile("" : "+v"(v_read[d]));
+    auto values = [&](uint32_t at, int ks) {  // of 16 keys and 32 coordinates, as an operand
+        const u32x2 v0 = lds_read_columns(at + ks * 16 * kRowBytes), v1 = lds_read_columns(at + (ks * 16 + 8) * kRowBytes);
+        return u32x4{v0.x, v0.y, v1.x, v1.y};
+    };
 
     f32x16 out[kBlocks];
 #pragma unroll
     for (int d = 0; d < kBlocks; ++d) out[d] = f32x16{};
     float top = kLowest, sum = 0.f;
 
-    // one tile; PART: some query of the wave does not see all of its keys
+    // one tile, at `buffer` of the room; PART: some query of the wave does not see all of its keys
     auto work_on = [&](int t, uint32_t buffer, auto part) {
         constexpr bool PART = decltype(part)::value;
         const int j0 = t * kTile;
-        f32x16 s[2];
+        uint32_t k_at[kKeyReads], v_at[kValueReads];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int x = 0; x < kKeyReads; ++x) asm("v_add_u32 %0, %1, %2" : "=v"(k_at[x]) : "s"(buffer), "v"(k_read[x]));
+#pragma unroll
+        for (int d = 0; d < kValueReads; ++d) asm("v_add_u32 %0, %1, %2" : "=v"(v_at[d]) : "s"(buffer), "v"(v_read[d]));
+        f32x16 s[kKeyBlocks];
+#pragma unroll
+        for (int kb = 0; kb < kKeyBlocks; ++kb) {
             s[kb] = f32x16{};
 #pragma unroll
-            for (int x = 0; x < D / 16; ++x)
-                s[kb] = T::mfma32(lds_read<u32x4>(buffer + k_read + kb * 32 * kRowBytes + (k_chunk ^ (2 * x)) * 16), q[x], s[kb]);
+            for (int x = 0; x < D / 16; ++x) s[kb] = T::mfma32(lds_read<u32x4>(k_at[x & 7] + (x >> 3) * 256 + kb * 32 * kRowBytes), q[x], s[kb]);
         }
-        // Where a score is a growing function of the product alone the largest product gives the largest score; otherwise the
-        // scores are made first.
-        constexpr bool kMade = PART || SLOPED;
-        float best = kMinusInf;
+        // register i of block kb is the key at j0 + 4 half + place(kb, i)
+        auto place = [](int kb, int i) { return 32 * kb + 8 * (i / 4) + i % 4; };
+        // the largest product or score, and for capped scores the largest magnitude
+        float best = kMinusInf, size = 0.f;
+        // Where the distance grows the score along the keys (all of them behind every query of the wave), slope * |i - j| is a
+        // part of the query and a part of the key.
+        const bool behind = SLOPED && !PART && j0 + kTile - 1 <= least_at;
+        const float bias = SLOPED ? slope * (float)(at - j0 - 4 * half) : 0.f;
+        if (SLOPED && behind) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < kKeyBlocks; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                if constexpr (kMade) {
-                    const int j = j0 + 32 * kb + 8 * (i / 4) + 4 * half + i % 4;
+                for (int i = 0; i < 16; ++i) {
+                    s[kb][i] = __builtin_fmaf(slope, (float)place(kb, i), score_of<CAP>(s[kb][i], rule));
+                    best = fmaxf(best, s[kb][i]);
+                }
+            best -= bias;
+        } else if (PART || SLOPED) {
+#pragma unroll
+            for (int kb = 0; kb < kKeyBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int j = j0 + 4 * half + place(kb, i);
                     float x = score_of<CAP>(s[kb][i], rule);
                     if constexpr (SLOPED) x = __builtin_fmaf(-slope, fabsf((float)(at - j)), x);
                     if constexpr (PART) x = j >= lo && j < hi ? x : kMinusInf;
                     s[kb][i] = x;
+                    best = fmaxf(best, x);
                 }
-                best = fmaxf(best, s[kb][i]);
-            }
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < kKeyBlocks; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    best = fmaxf(best, s[kb][i]);
+                    if constexpr (CAP) size = fmaxf(size, fabsf(s[kb][i]));
+                }
+        }
         best = max_halves(best);
-        if constexpr (!kMade) best = score_of<CAP>(best, rule);
+        if constexpr (!PART && !SLOPED) best = score_of<CAP>(best, rule);  // a growing function of the product
         // The reference of the exponentials follows the maximum only when it has fallen behind by more than kSlack: probabilities
         // then reach 2^kSlack, which both types hold as precisely as 1.
         if (__any(best > top + kSlack)) {
@@ -206,58 +250,64 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             for (int d = 0; d < kBlocks; ++d) out[d] *= f;
             top = next;
         }
-        u32x4 p[4];  // 16 keys each
+        u32x4 p[2 * kKeyBlocks];  // 16 keys each
         float more = 0.f;
+        auto exponentials = [&](auto score) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < kKeyBlocks; ++kb)
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                float e[2];
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-                    e[y] = __builtin_amdgcn_exp2f(kMade ? s[kb][i + y] - top : score_from<CAP>(s[kb][i + y], rule, top));
-                sum += e[0];
-                more += e[1];
-                p[2 * kb + i / 8][i % 8 / 2] = T::pack(e[0], e[1]);
-            }
+                for (int i = 0; i < 16; i += 2) {
+                    const float e0 = __builtin_amdgcn_exp2f(score(s[kb][i])), e1 = __builtin_amdgcn_exp2f(score(s[kb][i + 1]));
+                    sum += e0;
+                    more += e1;
+                    p[2 * kb + i / 8][i % 8 / 2] = T::pack(e0, e1);
+                }
+        };
+        if constexpr (PART || SLOPED) {
+            const float from = SLOPED && behind ? top + bias : top;
+            exponentials([&](float x) { return x - from; });
+        } else if constexpr (CAP) {
+            if (__any(size * rule.linear > kSmallTanh)) exponentials([&](float x) { return score_from<true>(x, rule, top); });
+            else exponentials([&](float x) { return small_score_from(x, rule, top); });
+        } else {
+            exponentials([&](float x) { return score_from<false>(x, rule, top); });
+        }
         sum += more;
         bool odd_values = false;
         if constexpr (PART) {
-            uint32_t odd = 0;
+            u16x2 largest = {0, 0};
+#pragma unroll 4
             for (int x = lane; x < kSlot / 16; x += 64) {
-                const u32x4 w = lds_read<u32x4>(buffer + kSlot + x * 16);
-                odd |= not_finite<T>(w.x) | not_finite<T>(w.y) | not_finite<T>(w.z) | not_finite<T>(w.w);
+                const u32x4 w = lds_read<u32x4>(all + buffer + kSlot + x * 16);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, w[y] & 0x7fff7fffu));
             }
-            odd_values = __any(odd != 0);
+            odd_values = __any(largest.x >= T::kExponent || largest.y >= T::kExponent);
         }
         if (!PART || !odd_values) {
 #pragma unroll
-            for (int ks = 0; ks < 4; ++ks)
+            for (int ks = 0; ks < 2 * kKeyBlocks; ++ks)
 #pragma unroll
-                for (int d = 0; d < kBlocks; ++d) {
-                    const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
-                    const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
-                    out[d] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p[ks], out[d]);
-                }
+                for (int d = 0; d < kBlocks; ++d) out[d] = T::mfma32(values(v_at[d & 3] + (d >> 2) * 256, ks), p[ks], out[d]);
         } else {
-            for (int ks = 0; ks < 4; ++ks) {
-                const u32x4 pk = ks == 0 ? p[0] : ks == 1 ? p[1] : ks == 2 ? p[2] : p[3];
+#pragma unroll
+            for (int ks = 0; ks < 2 * kKeyBlocks; ++ks)
 #pragma unroll
                 for (int d = 0; d < kBlocks; ++d) {
-                    const uint32_t c = buffer + v_read + ks * 16 * kRowBytes + (v_chunk ^ (4 * d)) * 16;
-                    const u32x2 v0 = lds_read_columns(c), v1 = lds_read_columns(c + 8 * kRowBytes);
-                    out[d] = T::mfma32(u32x4{v0.x & ~not_finite<T>(v0.x), v0.y & ~not_finite<T>(v0.y), v1.x & ~not_finite<T>(v1.x),
-                                             v1.y & ~not_finite<T>(v1.y)}, pk, out[d]);
+                    u32x4 v = values(v_at[d & 3] + (d >> 2) * 256, ks);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) v[w] &= ~not_finite<T>(v[w]);
+                    out[d] = T::mfma32(v, p[ks], out[d]);
                 }
-            }
             for (int y = 0; y < kTile; ++y) {
                 const bool seen = j0 + y >= lo && j0 + y < hi;
 #pragma unroll
                 for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t place = (4 * d + i) ^ R::value_turn32(y);
-                        const u32x2 w = lds_read<u32x2>(buffer + kSlot + y * kRowBytes + place * 16 + half * 8);
+                        const uint32_t chunk = (4 * d + i) ^ R::value_turn32(y);
+                        const u32x2 w = lds_read<u32x2>(all + buffer + kSlot + y * kRowBytes + chunk * 16 + half * 8);
                         const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
                         if (seen && (m.x & 0xffffu)) out[d][4 * i] += T::low(w.x);
                         if (seen && (m.x >> 16)) out[d][4 * i + 1] += T::high(w.x);
@@ -282,7 +332,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             request(next, all + ((t + 1 - t0) & 1) * (2 * kSlot));
             if (t + 2 < t1) next = find(t + 2);
         }
-        return all + ((t - t0) & 1) * (2 * kSlot);
+        return (uint32_t)((t - t0) & 1) * (2 * kSlot);
     };
     // The tiles that all queries of the wave see whole are a run; before and behind it, positions are compared.  Waves pass the
     // same number of barriers, whichever loop they are in.
@@ -376,7 +426,7 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     const int64_t tiles = rows / kTileRows + (c->n_seqs < n_tokens ? c->n_seqs : n_tokens), items = tiles * c->kv_heads;
     int64_t pieces = items > kAttnTickets ? 1 : ceil_div(kWantedWorkgroups, items);
     if (pieces > kMaxSplit) pieces = kMaxSplit;
-    if (pieces > ceil_div(max_len, 4 * kTile)) pieces = ceil_div(max_len, 4 * kTile);
+    if (pieces > ceil_div(max_len, 256)) pieces = ceil_div(max_len, 256);
     if (pieces < 1) pieces = 1;
     p.row_tiles = (int)tiles;
     p.n_split = (int)pieces;
