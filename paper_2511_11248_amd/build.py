@@ -13,7 +13,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtman.so")
 
 SOURCES = ["tman_abi.hip", "tman_tiling.hip", "tman_pack.hip", "tman_lut.hip", "tman_mpgemv.hip", "tman_mpgemv_i16.hip", "tman_mpgemv_x.hip", "tman_mpgemm.hip", "tman_mpgemm_small.hip", "tman_mpgemm_i8.hip", "tman_noalloc.hip",
-           "tman_attn_abi.hip", "tman_kv.hip", "tman_attn_decode.hip", "tman_attn_prefill.hip"]
+           "tman_attn_abi.hip", "tman_kv.hip", "tman_attn_decode.hip", "tman_attn_prefill.hip",
+           "tman_attn_prefill_few.hip"]
 
 # -packed-fp32-ops: keep the compiler from forming packed fp32 VALU instructions
 # kernarg-preload: scalar kernel arguments are in registers when a wave starts

@@ -50,12 +50,17 @@ struct DecodeArgs {
 };
 int launch_attn_decode(const DecodeArgs& a, hipStream_t st);
 
-// A prefill launch: a workgroup takes kRows rows - the new tokens of one sequence times the query heads of one key-value
-// head - and one piece of the positions.
+// A prefill launch: a workgroup takes some rows - the new tokens of one sequence times the query heads of one key-value head - and
+// one piece of the positions.  Few rows go to a kernel whose waves share out the positions (32 rows a workgroup, pieces meet as in
+// decoding), many to one whose waves share out the rows (128, pieces meet in a second kernel).
+constexpr int kFewRows = 32, kManyRows = 128;
 struct PrefillPlan {
+    int few;
     int row_tiles;  // at most, over all sequences
-    int n_split;
-    size_t partial_at, bytes;
+    int n_split;    // pieces, at most
+    int n_slots;    // of partial sums for an item (few)
+    int fold;       // the first so many workgroups of a key-value head take the last row tiles, from the last; the others from the first
+    size_t partial_at, count_at, bytes;
 };
 PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len);
 
@@ -72,11 +77,13 @@ struct PrefillArgs {
     int64_t q_stride, out_stride;
     int32_t* tickets;
     float* partial;
+    int32_t* counts;  // pieces of every item (many rows)
     float scale, cap;
     int heads, group, window, max_len, n_tokens;
     PrefillPlan p;
 };
 int launch_attn_prefill(const PrefillArgs& a, hipStream_t st);
+int launch_attn_prefill_few(const PrefillArgs& a, hipStream_t st);
 
 struct AppendArgs {
     KvView c;

@@ -167,6 +167,7 @@ int tman_attn_decode(const tman_kv_cache_t* cache, const tman_attn_t* attn, cons
 
 size_t tman_attn_prefill_workspace_bytes(const tman_kv_cache_t* cache, const tman_attn_t* attn, int32_t n_tokens, int32_t max_len) {
     if (check_cache_sizes(cache) != TMAN_OK || check_attn(cache, attn, max_len) != TMAN_OK || n_tokens < 1) return 0;
+    if ((int64_t)n_tokens * attn->heads > 0x7fffffff) return 0;
     return plan_attn_prefill(cache, attn, n_tokens, max_len).bytes;
 }
 
@@ -176,7 +177,7 @@ int tman_attn_prefill(const tman_kv_cache_t* cache, const tman_attn_t* attn, int
     int rc = check_cache(cache);
     if (rc != TMAN_OK) return rc;
     if ((rc = check_attn(cache, attn, max_len)) != TMAN_OK) return rc;
-    if (n_tokens < 1) return TMAN_ERR_SHAPE;
+    if (n_tokens < 1 || (int64_t)n_tokens * attn->heads > 0x7fffffff) return TMAN_ERR_SHAPE;
     if (!lens || !q_start) return TMAN_ERR_NULL;
     if ((rc = check_rows(q, q_stride, attn->heads, cache->dim)) != TMAN_OK) return rc;
     if ((rc = check_rows(out, out_stride, attn->heads, cache->dim)) != TMAN_OK) return rc;
@@ -201,6 +202,7 @@ int tman_attn_prefill(const tman_kv_cache_t* cache, const tman_attn_t* attn, int
     if (a.p.bytes) {
         a.tickets = reinterpret_cast<int32_t*>(ws);
         a.partial = reinterpret_cast<float*>(ws + a.p.partial_at);
+        a.counts = reinterpret_cast<int32_t*>(ws + a.p.count_at);
     }
     a.scale = attn->scale;
     a.cap = attn->cap;

@@ -10,7 +10,7 @@
 //     any exchange, the operand that P^T has to be in out^T = V^T P^T - the keys of a product may come in any order as
 //     long as V^T has the same, and V^T is read from LDS by columns in just that order.
 //   * Groups of fewer than 16 heads leave columns idle, which costs nothing here: the products take a tenth of the time.
-#include "tman_attn_device.h"
+#include "tman_attn_join.h"
 
 namespace tman {
 namespace {
@@ -19,27 +19,12 @@ constexpr int kTile = 32;   // positions a wave takes at once
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 constexpr int kHeads = 16;  // query heads of a workgroup, at most
-constexpr int kMaxSplit = 256;
-constexpr int kAtOnce = 8;  // pieces that a thread of the join reads at once
-constexpr int kGroup = 32;  // pieces that meet at once
-
-// [row item][piece]: heads x D sums, then the maxima and the sums of probabilities
-__host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kHeads * D + 2 * kHeads; }
-
-__device__ __forceinline__ void store_shared(float* p, float x, float y) {
-    const u32x2 w = {__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, w), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ f32x2 load_shared(const float* p) {
-    return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
-
 template <class T, int D, bool CAP, bool WEIGHTS>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel(DecodeArgs a) {
     using R = RowsOf<D>;
     constexpr int kRowBytes = R::kBytes, kSlot = kTile * kRowBytes, kRequests = kSlot / 1024, kHalf = kRequests / 2;
-    constexpr int kOut = D + 4;  // floats from one head's sums to the next's in LDS
-    constexpr int kWaveBytes = 2 * kSlot > kHeads * kOut * 4 ? 2 * kSlot : kHeads * kOut * 4;
+    using Meet = Join<D, kHeads, kWaves>;
+    constexpr int kWaveBytes = 2 * kSlot > Meet::kWaveBytes ? 2 * kSlot : Meet::kWaveBytes;
     __shared__ __attribute__((aligned(1024))) uint8_t room[kWaves * kWaveBytes];
     __shared__ float wave_max[kWaves][kHeads], wave_sum[kWaves][kHeads];
     __shared__ int last;
@@ -204,11 +189,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
         wave_sum[wave][col] = sum;
     }
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d) lds_write(mine + (col * kOut + 16 * d + 4 * g) * 4, out[d]);
+    for (int d = 0; d < D / 16; ++d) lds_write(mine + (col * Meet::kStride + 16 * d + 4 * g) * 4, out[d]);
     __syncthreads();
 
-    const int64_t item = ((int64_t)b * a.c.kv_heads + hk) * a.p.head_chunks + chunk;
-    float* partial = a.partial + (item * a.p.n_slots + blockIdx.x) * partial_floats(D);
     const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
     auto finish = [&](int h, int d, float m, float l, f32x4 o) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -220,113 +203,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
             if constexpr (WEIGHTS) a.lse2[(int64_t)b * a.heads + h0 + h] = l == 0.f ? kMinusInf : l2;
         }
     };
-    auto publish = [&](float* to, int h, int d, float m, float l, f32x4 o) {
-        store_shared(to + h * D + d, o[0], o[1]);
-        store_shared(to + h * D + d + 2, o[2], o[3]);
-        if (d == 0) store_shared(to + kHeads * D + 2 * h, m, l);
-    };
-    for (int x = threadIdx.x; x < n_heads * (D / 4); x += kThreads) {
-        const int h = x / (D / 4), d = x % (D / 4) * 4;
-        float m = wave_max[0][h];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, wave_max[w][h]);
-        float l = 0.f;
-        f32x4 o = {0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(wave_max[w][h] - m);
-            l = __builtin_fmaf(f, wave_sum[w][h], l);
-            o += f * lds_read<f32x4>(all + w * kWaveBytes + (h * kOut + d) * 4);
-        }
-        if (pieces == 1) {
-            finish(h, d, m, l, o);
-        } else {
-            publish(partial, h, d, m, l, o);
-        }
-    }
-    if (pieces == 1) return;
-
-    // The last piece to arrive adds them up, in the order of the pieces; many pieces meet in groups first, whose last ones meet.
-    // A thread takes four coordinates of a head and every kShares-th piece, with the reads of several pieces under way at once; the
-    // shares then meet in LDS.
-    float* base = a.partial + item * a.p.n_slots * partial_floats(D);
-    const int quads = n_heads * (D / 4);
-    auto arrive = [&](int32_t* ticket, int of) {  // whether this workgroup is the last; its sums have reached coherent memory
-        wait_requests<0>();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
-            if (last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        return last != 0;
-    };
-    auto join = [&](int first, int count, auto done) {
-        int shares = 1;
-        while (shares * 2 * quads <= kThreads && shares * kAtOnce < count) shares *= 2;
-        for (int x = threadIdx.x; x < quads * shares; x += kThreads) {
-            const int share = x / quads, y = x - share * quads, h = y / (D / 4), d = y % (D / 4) * 4;
-            float m = kLowest, l = 0.f;
-            f32x4 o = {0, 0, 0, 0};
-            for (int p0 = share; p0 < count; p0 += kAtOnce * shares) {
-                f32x2 ml[kAtOnce], v[kAtOnce][2];
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const float* from = base + (first + min(p0 + k * shares, count - 1)) * partial_floats(D);
-                    ml[k] = load_shared(from + kHeads * D + 2 * h);
-                    v[k][0] = load_shared(from + h * D + d);
-                    v[k][1] = load_shared(from + h * D + d + 2);
-                }
-                float next = m;
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
-                const float f = __builtin_amdgcn_exp2f(m - next);
-                l *= f;
-                o *= f;
-                m = next;
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    if (p0 + k * shares >= count) continue;
-                    const float e = __builtin_amdgcn_exp2f(ml[k].x - m);
-                    l = __builtin_fmaf(e, ml[k].y, l);
-                    o += e * f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y};
-                }
-            }
-            if (shares > 1) {
-                lds_write(all + x * 16, o);
-                lds_write(all + kThreads * 16 + x * 8, f32x2{m, l});
-            } else {
-                done(h, d, m, l, o);
-            }
-        }
-        if (shares == 1) return;
-        __syncthreads();
-        for (int y = threadIdx.x; y < quads; y += kThreads) {
-            const int h = y / (D / 4), d = y % (D / 4) * 4;
-            float m = kLowest, l = 0.f;
-            f32x4 o = {0, 0, 0, 0};
-            for (int s = 0; s < shares; ++s) m = fmaxf(m, lds_read<f32x2>(all + kThreads * 16 + (s * quads + y) * 8).x);
-            for (int s = 0; s < shares; ++s) {
-                const f32x2 ml = lds_read<f32x2>(all + kThreads * 16 + (s * quads + y) * 8);
-                const float e = __builtin_amdgcn_exp2f(ml.x - m);
-                l = __builtin_fmaf(e, ml.y, l);
-                o += e * lds_read<f32x4>(all + (s * quads + y) * 16);
-            }
-            done(h, d, m, l, o);
-        }
-    };
-    int32_t* tickets = a.tickets + item * (1 + a.p.n_slots - a.p.n_split);
-    if (pieces <= kGroup) {
-        if (arrive(tickets, pieces)) join(0, pieces, finish);
+    if (pieces == 1) {
+        Meet::waves(all, kWaveBytes, wave_max, wave_sum, n_heads, finish);
         return;
     }
-    const int group = (int)blockIdx.x / kGroup, groups = (pieces + kGroup - 1) / kGroup;
-    const int members = min(kGroup, pieces - group * kGroup);
-    if (!arrive(tickets + 1 + group, members)) return;
-    join(group * kGroup, members, [&](int h, int d, float m, float l, f32x4 o) {
-        publish(base + (a.p.n_split + group) * partial_floats(D), h, d, m, l, o);
+    const int64_t item = ((int64_t)b * a.c.kv_heads + hk) * a.p.head_chunks + chunk;
+    float* base = a.partial + item * a.p.n_slots * Meet::kSlotFloats;
+    Meet::waves(all, kWaveBytes, wave_max, wave_sum, n_heads, [&](int h, int d, float m, float l, f32x4 o) {
+        Meet::publish(base + blockIdx.x * Meet::kSlotFloats, h, d, m, l, o);
     });
-    if (arrive(tickets, groups)) join(a.p.n_split, groups, finish);
+    Meet::pieces(base, a.tickets + item * (1 + a.p.n_slots - a.p.n_split), blockIdx.x, pieces, a.p.n_split, n_heads, all, &last, finish);
 }
 
 // Accumulated weights: once a row's sum is known, its probabilities come out of the kept scores; a thread adds those of the heads of
@@ -395,15 +281,15 @@ DecodePlan plan_attn_decode(const tman_kv_cache_t* c, const tman_attn_t* a, int 
     const int seen = a->window > 0 && a->window < max_len ? a->window : max_len;
     const int tiles = ceil_div(seen, kTile) + (seen < max_len ? 1 : 0);  // a window may start inside a tile
     int pieces = rows > kAttnTickets ? 1 : ceil_div(kWantedWorkgroups, rows);
-    if (pieces > kMaxSplit) pieces = kMaxSplit;
+    if (pieces > kMaxPieces) pieces = kMaxPieces;
     if (pieces > ceil_div(tiles, kLeastTiles)) pieces = ceil_div(tiles, kLeastTiles);
     if (pieces < 1) pieces = 1;
     p.split_tiles = ceil_div(tiles, pieces);
     p.n_split = pieces;  // (as many as room is kept for: a longer max_len never needs less)
-    p.n_slots = pieces + (pieces > kGroup ? ceil_div(pieces, kGroup) : 0);
+    p.n_slots = piece_slots(pieces);
     p.score_stride = ceil_div(max_len, kTile) * kTile;
     p.partial_at = kAttnTicketBytes;
-    p.score_at = p.partial_at + (pieces > 1 ? rows * p.n_slots * partial_floats(c->dim) * sizeof(float) : 0);
+    p.score_at = p.partial_at + (pieces > 1 ? rows * p.n_slots * ((size_t)kHeads * c->dim + 2 * kHeads) * sizeof(float) : 0);
     p.lse_at = p.score_at + (weights ? (size_t)c->n_seqs * a->heads * p.score_stride * sizeof(float) : 0);
     p.bytes = p.lse_at + (weights ? (size_t)c->n_seqs * a->heads * sizeof(float) : 0);
     return p;

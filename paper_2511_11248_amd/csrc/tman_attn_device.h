@@ -139,13 +139,11 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 struct ScoreRule {
     float scale;       // scale * log2 e, capped: 2 scale log2 e / cap
     float cap;         // cap * log2 e, or 0
-    float linear;      // capped: scale / cap
-    float p[5];        // capped: cap * log2 e times the coefficients of tanh(x) / x in x^2
     __device__ __forceinline__ ScoreRule(float s, float c)
-        : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e), linear(c > 0.f ? s / c : 0.f),
-          p{cap * 0.99999993f, cap * -0.33332302f, cap * 0.13310064f, cap * -0.05209665f, cap * 0.01546875f} {}
+        : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e) {}
 };
-// cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of 2^-23 cap, whatever x.
+// cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of 2^-23 cap, whatever x.  (exp2 and the reciprocal take the time of two
+// products each here, so a polynomial for small x is no faster: six products more in their place gave the same times.)
 template <bool CAP>
 __device__ __forceinline__ float score_of(float raw, const ScoreRule& r) {
     if constexpr (!CAP) return raw * r.scale;
@@ -159,18 +157,6 @@ __device__ __forceinline__ float score_from(float raw, const ScoreRule& r, float
     const float e = __builtin_amdgcn_exp2f(raw * r.scale);
     return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap - top);
 }
-// ... and without the exponential and the reciprocal, each of which takes the time of four products: for |x| up to
-// kSmallTanh an interpolation at the Chebyshev points, off by 8e-8 of the result at most.
-constexpr float kSmallTanh = 0.6f;
-__device__ __forceinline__ float small_score_from(float raw, const ScoreRule& r, float top) {
-    const float x = raw * r.linear, u = x * x;
-    float f = __builtin_fmaf(u, r.p[4], r.p[3]);
-    f = __builtin_fmaf(u, f, r.p[2]);
-    f = __builtin_fmaf(u, f, r.p[1]);
-    f = __builtin_fmaf(u, f, r.p[0]);
-    return __builtin_fmaf(x, f, -top);
-}
-
 // Rows of keys and values in LDS.  A request (one wave, 64 x 16 bytes straight into LDS) brings 1024 bytes, whole rows; lane l's 16 bytes
 // land at 16 l of it, so an arrangement that keeps the reads off each other's banks is made by choosing which bytes a lane asks for:
 // chunk c (16 bytes) of row r is kept at place c ^ key_turn(r), or c ^ value_turn(r).
@@ -185,5 +171,112 @@ struct RowsOf {
     // ... or 64 bytes of each of 4 rows (of a 32-column product)
     static constexpr __host__ __device__ uint32_t value_turn32(uint32_t r) { return (D == 64 ? (r >> 1) & 1 : r & 3) << 2; }
 };
+
+// Rows of a prompt's launch: the new tokens of a sequence times the query heads of a key-value head, in tiles of ROWS rows, all
+// sequences' tiles one after another.
+struct RowTile {
+    int b;       // sequence, -1: there is no such tile
+    int tile;    // of the sequence
+    int start, tokens;
+};
+template <int ROWS>
+__device__ __forceinline__ RowTile find_row_tile(const PrefillArgs& a, int item, int lane) {
+    RowTile r = {-1, item, 0, 0};
+    for (int at = 0; at < a.c.n_seqs; at += 64) {
+        int s0 = 0, n = 0;
+        if (at + lane < a.c.n_seqs) {
+            s0 = min(max(a.q_start[at + lane], 0), a.n_tokens);
+            n = min(max(a.q_start[at + lane + 1], s0), a.n_tokens) - s0;
+        }
+        const int tiles = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
+        int run = tiles;
+        if (a.c.n_seqs > 1) {
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(run, d);
+                if (lane >= d) run += other;
+            }
+        }
+        const uint64_t found = __ballot(run > r.tile);
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            r.b = at + l;
+            r.tile -= __builtin_amdgcn_readlane(run - tiles, l);
+            r.start = __builtin_amdgcn_readlane(s0, l);
+            r.tokens = __builtin_amdgcn_readlane(n, l);
+            return r;
+        }
+        r.tile -= __builtin_amdgcn_readlane(run, 63);
+    }
+    return r;
+}
+
+// One row: token n at position `at`, query head `head`; it sees the keys of [lo, hi).
+struct QueryRow {
+    bool valid, sees;
+    int n, head, at, lo, hi;
+};
+__device__ __forceinline__ int lowest_seen(const PrefillArgs& a, int at) { return a.window > 0 ? max(0, at + 1 - a.window) : 0; }
+__device__ __forceinline__ QueryRow query_row(const PrefillArgs& a, const RowTile& t, int64_t row, int hk, int len) {
+    QueryRow r;
+    r.valid = row < (int64_t)t.tokens * a.group;
+    const int x = r.valid ? (int)row : 0, token = x / a.group;
+    r.head = hk * a.group + x - token * a.group;
+    r.n = t.start + token;
+    r.at = len - t.tokens + token;
+    r.lo = lowest_seen(a, r.at);
+    r.hi = r.at + 1;
+    if (a.first) r.lo = max(r.lo, a.first[r.n]);
+    if (a.end) r.hi = a.end[r.n];
+    r.hi = min(r.hi, len);
+    r.sees = r.valid && r.lo < r.hi;
+    return r;
+}
+
+// Of some rows that see something: all that any of them sees lies in [least, most), all of them see [inner_lo, inner_hi), none is at
+// a position before least_at.
+struct Span {
+    int least, most, inner_lo, inner_hi, least_at;
+};
+__device__ __forceinline__ int min_of_columns(int x) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) x = min(x, __shfl_xor(x, d));
+    return scalar(x);
+}
+constexpr int kNoPosition = 0x7fffffff;
+__device__ __forceinline__ Span span_of_columns(const QueryRow& r) {  // of the wave's 32 columns
+    return Span{min_of_columns(r.sees ? r.lo : kNoPosition), -min_of_columns(r.sees ? -r.hi : 0), -min_of_columns(r.sees ? -r.lo : 0),
+                min_of_columns(r.sees ? r.hi : kNoPosition), min_of_columns(r.sees ? r.at : kNoPosition)};
+}
+// The same of rows row0 to row0 + count - 1 where no intervals are given: bounds grow with the position, so the first and the last
+// row say it all.
+__device__ __forceinline__ Span span_of_rows(const PrefillArgs& a, const RowTile& t, int64_t row0, int count, int len) {
+    const int64_t rows = (int64_t)t.tokens * a.group;
+    const int before = len - t.tokens;
+    Span s = {kNoPosition, 0, 0, kNoPosition, kNoPosition};
+    if (row0 >= rows) return s;
+    const int last = before + (int)((row0 + count < rows ? row0 + count : rows) - 1) / a.group;
+    if (last < 0) return s;  // more tokens than positions
+    const int first = max(before + (int)row0 / a.group, 0);
+    s.least = lowest_seen(a, first);
+    s.inner_lo = lowest_seen(a, last);
+    s.most = last + 1;
+    s.inner_hi = first + 1;
+    s.least_at = first;
+    return s;
+}
+
+// the elements of w that are not finite, as all ones
+template <class T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+    constexpr uint32_t e = T::kExponent;
+    return ((w & e) == e ? 0xffffu : 0u) | ((w & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
+}
+// the larger of what `largest` holds and the magnitudes' bits of eight elements; not finite ones are at least T::kExponent
+__device__ __forceinline__ u16x2 larger_bits(u16x2 largest, u32x4 w) {
+#pragma unroll
+    for (int y = 0; y < 4; ++y) largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, w[y] & 0x7fff7fffu));
+    return largest;
+}
 
 }  // namespace tman

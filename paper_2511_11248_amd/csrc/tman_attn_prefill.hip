@@ -13,41 +13,35 @@
 //     where it is seen.
 #include <type_traits>
 
-#include "tman_attn_device.h"
+#include "tman_attn_join.h"
 
 namespace tman {
 namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * 64;
-constexpr int kTileRows = kWaves * 32;
 constexpr int kMaxSplit = 64;
+static_assert(kManyRows == kWaves * 32, "a wave takes 32 rows");
 constexpr float kSlack = 8.f;
+constexpr int kLeastTiles = 4;  // of a piece
 
 // Positions of a tile: heads of 256 leave registers for the scores of 32.
 __host__ __device__ constexpr int tile_of(int D) { return D == 256 ? 32 : 64; }
 
-// [item][piece]: every wave's accumulators as they lie in its lanes, then its maxima and sums
-__host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kTileRows * D + 2 * kTileRows; }
+// [item][piece]: every wave's accumulators as they lie in its lanes, then the maxima and sums of its columns
+__host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kManyRows * D + 2 * kManyRows; }
 
-__device__ __forceinline__ void store_shared(float* p, float x, float y) {
-    const u32x2 w = {__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, y)};
-    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, w), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ f32x2 load_shared(const float* p) {
-    return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
-}
+// the row tile of workgroup number r of a key-value head (and piece)
+__device__ __forceinline__ int item_of(const PrefillPlan& p, int r) { return r < p.fold ? p.row_tiles - 1 - r : r - p.fold; }
 
-__device__ __forceinline__ int min_of_columns(int x) {
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) x = min(x, __shfl_xor(x, d));
-    return scalar(x);
-}
-
-// the elements of w that are not finite, as all ones
+// 32 coordinates of a row: register 4 i + x of a lane is coordinate 8 i + 4 half + x
 template <class T>
-__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
-    constexpr uint32_t e = T::kExponent;
-    return ((w & e) == e ? 0xffffu : 0u) | ((w & (e << 16)) == (e << 16) ? 0xffff0000u : 0u);
+__device__ __forceinline__ void store_block(uint8_t* to, const f32x16& out, float inv, bool empty, int half) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        u32x2 w = {T::pack(out[4 * i] * inv, out[4 * i + 1] * inv), T::pack(out[4 * i + 2] * inv, out[4 * i + 3] * inv)};
+        if (empty) w = u32x2{0, 0};  // nothing seen, or nothing of any weight
+        *reinterpret_cast<u32x2*>(to + (8 * i + 4 * half) * 2) = w;
+    }
 }
 
 template <class T, int D, bool CAP, bool SLOPED>
@@ -59,73 +53,50 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     constexpr int kRequests = kOwnRows * kRowBytes / 1024;              // and as many requests for the values
     constexpr int kBlocks = D / 32;
     __shared__ __attribute__((aligned(1024))) uint8_t room[2 * 2 * kSlot];
-    __shared__ int wave_lo[kWaves], wave_hi[kWaves], last;
+    __shared__ Span wave_span[kWaves];
+    __shared__ __attribute__((aligned(16))) uint32_t odd_rows[2][kWaves];  // of a buffer's values: those that a wave requested are not all finite
 
     const int wave = scalar((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int col = lane & 31, half = lane >> 5;
 
     // which rows: the heaviest (the last) first, key-value heads over the XCDs
     const int hk = (int)blockIdx.x % a.c.kv_heads, rest = (int)blockIdx.x / a.c.kv_heads;
-    const int piece = rest % a.p.n_split, item = a.p.row_tiles - 1 - rest / a.p.n_split;
-    int b = -1, tile = item, start = 0, tokens = 0;
-    for (int at = 0; at < a.c.n_seqs && b < 0; at += 64) {
-        int s0 = 0, n = 0;
-        if (at + lane < a.c.n_seqs) {
-            s0 = min(max(a.q_start[at + lane], 0), a.n_tokens);
-            n = min(max(a.q_start[at + lane + 1], s0), a.n_tokens) - s0;
-        }
-        const int tiles = (int)(((int64_t)n * a.group + kTileRows - 1) / kTileRows);
-        int run = tiles;
+    const int piece = rest % a.p.n_split, item = item_of(a.p, rest / a.p.n_split);
+    const RowTile rows = find_row_tile<kManyRows>(a, item, lane);
+    if (rows.b < 0) {
+        if (a.p.n_split > 1 && piece == 0 && threadIdx.x == 0) a.counts[(int64_t)item * a.c.kv_heads + hk] = 0;
+        return;
+    }
+    const int b = rows.b, len = checked_length(a.c, a.lens, b, a.max_len);
+    if (rows.tokens > len && threadIdx.x == 0) report_index_error(a.c.status);
+    const int64_t row0 = (int64_t)rows.tile * kManyRows;
+    const QueryRow r = query_row(a, rows, row0 + wave * 32 + col, hk, len);
+    const int at = r.at, lo = r.lo, hi = r.hi, n = r.n, head = r.head;
+    Span span, whole;  // of the wave, and of all rows
+    if (a.first || a.end) {
+        span = span_of_columns(r);
+        if (lane == 0) wave_span[wave] = span;
+        __syncthreads();
+        whole = wave_span[0];
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int other = __shfl_up(run, d);
-            if (lane >= d) run += other;
+        for (int w = 1; w < kWaves; ++w) {
+            whole.least = min(whole.least, wave_span[w].least);
+            whole.most = max(whole.most, wave_span[w].most);
+            whole.inner_lo = max(whole.inner_lo, wave_span[w].inner_lo);
+            whole.inner_hi = min(whole.inner_hi, wave_span[w].inner_hi);
         }
-        const uint64_t found = __ballot(run > tile);
-        if (found) {
-            const int l = __builtin_ctzll(found);
-            b = at + l;
-            tile -= __builtin_amdgcn_readlane(run - tiles, l);
-            start = __builtin_amdgcn_readlane(s0, l);
-            tokens = __builtin_amdgcn_readlane(n, l);
-        } else {
-            tile -= __builtin_amdgcn_readlane(run, 63);
-        }
+    } else {
+        span = span_of_rows(a, rows, row0 + wave * 32, 32, len);
+        whole = span_of_rows(a, rows, row0, kManyRows, len);
     }
-    if (b < 0) return;
-    const int len = checked_length(a.c, a.lens, b, a.max_len);
-    if (tokens > len && threadIdx.x == 0) report_index_error(a.c.status);
-
-    // the lane's row: a token and a query head, and the interval [lo, hi) that it sees
-    const int64_t row64 = (int64_t)tile * kTileRows + wave * 32 + col;
-    const bool valid = row64 < (int64_t)tokens * a.group;
-    const int row = valid ? (int)row64 : 0;
-    const int token = row / a.group, head = hk * a.group + row - token * a.group;
-    const int n = start + token, at = len - tokens + token;
-    int lo = 0, hi = at + 1;
-    if (a.first) lo = max(a.first[n], 0);
-    if (a.end) hi = a.end[n];
-    if (a.window > 0) lo = max(lo, at + 1 - a.window);
-    hi = min(hi, len);
-    const bool sees = valid && lo < hi;
-    // of the wave: everything that is seen lies in [least, most), what all see in [inner_lo, inner_hi)
-    const int least = min_of_columns(sees ? lo : 0x7fffffff), most = -min_of_columns(sees ? -hi : 0);
-    const int inner_lo = -min_of_columns(sees ? -lo : 0), inner_hi = min_of_columns(sees ? hi : 0x7fffffff);
-    const int least_at = min_of_columns(sees ? at : 0x7fffffff);
-    if (lane == 0) {
-        wave_lo[wave] = least;
-        wave_hi[wave] = most;
-    }
-    __syncthreads();
-    int all_lo = 0x7fffffff, all_hi = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        all_lo = min(all_lo, scalar(wave_lo[w]));
-        all_hi = max(all_hi, scalar(wave_hi[w]));
-    }
-    const int first_tile = all_lo < all_hi ? all_lo / kTile : 0, n_tiles = all_lo < all_hi ? (all_hi + kTile - 1) / kTile - first_tile : 0;
-    const int per_piece = (n_tiles + a.p.n_split - 1) / a.p.n_split;
-    const int pieces = per_piece > 0 ? (n_tiles + per_piece - 1) / per_piece : 1;
+    const bool some = scalar(whole.least) < scalar(whole.most);
+    const int first_tile = some ? scalar(whole.least) / kTile : 0, n_tiles = some ? (scalar(whole.most) + kTile - 1) / kTile - first_tile : 0;
+    const int all_lo = scalar(whole.inner_lo), all_hi = scalar(whole.inner_hi);  // all rows see whole tiles between them
+    const int least = scalar(span.least), most = scalar(span.most), inner_lo = scalar(span.inner_lo), inner_hi = scalar(span.inner_hi);
+    const int least_at = scalar(span.least_at);
+    const int per_piece = max((n_tiles + a.p.n_split - 1) / a.p.n_split, kLeastTiles);
+    const int pieces = max((n_tiles + per_piece - 1) / per_piece, 1);
+    if (a.p.n_split > 1 && piece == 0 && threadIdx.x == 0) a.counts[(int64_t)item * a.c.kv_heads + hk] = pieces;
     if (piece >= pieces) return;
     const int t0 = first_tile + piece * per_piece, t1 = min(first_tile + n_tiles, t0 + per_piece);
 
@@ -203,8 +174,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         }
         // register i of block kb is the key at j0 + 4 half + place(kb, i)
         auto place = [](int kb, int i) { return 32 * kb + 8 * (i / 4) + i % 4; };
-        // the largest product or score, and for capped scores the largest magnitude
-        float best = kMinusInf, size = 0.f;
+        float best = kMinusInf;  // the largest product or score
         // Where the distance grows the score along the keys (all of them behind every query of the wave), slope * |i - j| is a
         // part of the query and a part of the key.
         const bool behind = SLOPED && !PART && j0 + kTile - 1 <= least_at;
@@ -234,10 +204,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
 #pragma unroll
             for (int kb = 0; kb < kKeyBlocks; ++kb)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    best = fmaxf(best, s[kb][i]);
-                    if constexpr (CAP) size = fmaxf(size, fabsf(s[kb][i]));
-                }
+                for (int i = 0; i < 16; ++i) best = fmaxf(best, s[kb][i]);
         }
         best = max_halves(best);
         if constexpr (!PART && !SLOPED) best = score_of<CAP>(best, rule);  // a growing function of the product
@@ -266,24 +233,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         if constexpr (PART || SLOPED) {
             const float from = SLOPED && behind ? top + bias : top;
             exponentials([&](float x) { return x - from; });
-        } else if constexpr (CAP) {
-            if (__any(size * rule.linear > kSmallTanh)) exponentials([&](float x) { return score_from<true>(x, rule, top); });
-            else exponentials([&](float x) { return small_score_from(x, rule, top); });
         } else {
-            exponentials([&](float x) { return score_from<false>(x, rule, top); });
+            exponentials([&](float x) { return score_from<CAP>(x, rule, top); });
         }
         sum += more;
         bool odd_values = false;
         if constexpr (PART) {
-            u16x2 largest = {0, 0};
-#pragma unroll 4
-            for (int x = lane; x < kSlot / 16; x += 64) {
-                const u32x4 w = lds_read<u32x4>(all + buffer + kSlot + x * 16);
-#pragma unroll
-                for (int y = 0; y < 4; ++y)
-                    largest = __builtin_elementwise_max(largest, __builtin_bit_cast(u16x2, w[y] & 0x7fff7fffu));
-            }
-            odd_values = __any(largest.x >= T::kExponent || largest.y >= T::kExponent);
+            const u32x4 f = *reinterpret_cast<const u32x4*>(odd_rows[(t - t0) & 1]);
+            odd_values = scalar((int)(f.x | f.y | f.z | f.w)) != 0;
         }
         if (!PART || !odd_values) {
 #pragma unroll
@@ -325,6 +282,14 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     }
     auto enter = [&](int t) {  // tile t is there, its buffer's neighbour is free and takes the next one
         wait_requests<0>();
+        if (t * kTile < all_lo || (t + 1) * kTile > all_hi) {  // somebody compares positions: are all values finite?
+            u16x2 largest = {0, 0};
+#pragma unroll
+            for (int i = 0; i < kRequests; ++i)
+                largest = larger_bits(largest, lds_read<u32x4>(all + ((t - t0) & 1) * (2 * kSlot) + kSlot + (wave * kRequests + i) * 1024 + lane * 16));
+            const bool odd = __any(largest.x >= T::kExponent || largest.y >= T::kExponent);
+            if (lane == 0) odd_rows[(t - t0) & 1][wave] = odd;
+        }
         wait_lds();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -348,61 +313,74 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     }
     sum = sum_halves(sum);
 
-    if (pieces > 1) {
-        // the pieces meet in the workspace; the last to arrive adds them up in their order
-        const int64_t group_item = (int64_t)item * a.c.kv_heads + hk;
-        float* base = a.partial + group_item * a.p.n_split * partial_floats(D);
-        const bool any = __any(valid);
-        if (any) {
-            float* mine = base + piece * partial_floats(D);
+    if (pieces > 1) {  // a second kernel adds the pieces up
+        if (!__any(r.valid)) return;
+        float* mine = a.partial + (((int64_t)item * a.c.kv_heads + hk) * a.p.n_split + piece) * partial_floats(D);
 #pragma unroll
-            for (int d = 0; d < kBlocks; ++d)
+        for (int d = 0; d < kBlocks; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; i += 2)
-                    store_shared(mine + (((wave * kBlocks + d) * 8 + i / 2) * 64 + lane) * 2, out[d][i], out[d][i + 1]);
-            if (half == 0) store_shared(mine + kTileRows * D + (wave * 32 + col) * 2, top, sum);
-        }
-        wait_requests<0>();
-        __syncthreads();
-        if (threadIdx.x == 0) last = __hip_atomic_fetch_add(a.tickets + group_item, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pieces - 1;
-        __syncthreads();
-        if (!last) return;
-        if (threadIdx.x == 0) __hip_atomic_store(a.tickets + group_item, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (!any) return;
-        top = kLowest;
-        for (int p = 0; p < pieces; ++p) top = fmaxf(top, load_shared(base + p * partial_floats(D) + kTileRows * D + (wave * 32 + col) * 2).x);
-        sum = 0.f;
-#pragma unroll
-        for (int d = 0; d < kBlocks; ++d) out[d] = f32x16{};
-        for (int p = 0; p < pieces; ++p) {
-            const float* from = base + p * partial_floats(D);
-            const f32x2 ml = load_shared(from + kTileRows * D + (wave * 32 + col) * 2);
-            const float f = __builtin_amdgcn_exp2f(ml.x - top);
-            sum = __builtin_fmaf(f, ml.y, sum);
-#pragma unroll
-            for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; i += 2) {
-                    const f32x2 v = load_shared(from + (((wave * kBlocks + d) * 8 + i / 2) * 64 + lane) * 2);
-                    out[d][i] = __builtin_fmaf(f, v.x, out[d][i]);
-                    out[d][i + 1] = __builtin_fmaf(f, v.y, out[d][i + 1]);
-                }
-        }
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4*>(mine + (((wave * kBlocks + d) * 4 + i) * 64 + lane) * 4) =
+                    f32x4{out[d][4 * i], out[d][4 * i + 1], out[d][4 * i + 2], out[d][4 * i + 3]};
+        if (half == 0) *reinterpret_cast<f32x2*>(mine + kManyRows * D + (wave * 32 + col) * 2) = f32x2{top, sum};
+        return;
     }
-
-    if (!valid) return;
-    const bool empty = !sees || sum == 0.f;
+    if (!r.valid) return;
+    const bool empty = !r.sees || sum == 0.f;
     const float inv = empty ? 0.f : 1.f / sum;
     uint8_t* to = a.out + (n * a.out_stride + (int64_t)head * D) * 2;
 #pragma unroll
-    for (int d = 0; d < kBlocks; ++d)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            u32x2 w = {T::pack(out[d][4 * i] * inv, out[d][4 * i + 1] * inv), T::pack(out[d][4 * i + 2] * inv, out[d][4 * i + 3] * inv)};
-            if (empty) w = u32x2{0, 0};
-            *reinterpret_cast<u32x2*>(to + (32 * d + 8 * i + 4 * half) * 2) = w;
-        }
+    for (int d = 0; d < kBlocks; ++d) store_block<T>(to + 64 * d, out[d], inv, empty, half);
     if (a.lse && half == 0) a.lse[(int64_t)n * a.heads + head] = empty ? kMinusInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// The pieces of an item's rows, 32 coordinates at a time: a wave takes the lanes' sums as they were left, four pieces under way at once.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void attn_prefill_join_kernel(PrefillArgs a) {
+    constexpr int kBlocks = D / 32, kAtOnce = 4;
+    const int wave = scalar((int)threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+    const int d = (int)blockIdx.x % kBlocks, rest = (int)blockIdx.x / kBlocks, hk = rest % a.c.kv_heads, item = rest / a.c.kv_heads;
+    const int64_t at = (int64_t)item * a.c.kv_heads + hk;
+    const int pieces = scalar_load(a.counts, at);
+    if (pieces <= 1) return;
+    const RowTile rows = find_row_tile<kManyRows>(a, item, lane);
+    if (rows.b < 0) return;
+    const int len = checked_length(a.c, a.lens, rows.b, a.max_len);
+    const QueryRow r = query_row(a, rows, (int64_t)rows.tile * kManyRows + wave * 32 + col, hk, len);
+    if (!__any(r.valid)) return;
+    const float* base = a.partial + at * a.p.n_split * partial_floats(D);
+    float top = kLowest, sum = 0.f;
+    f32x16 out = {};
+    for (int p0 = 0; p0 < pieces; p0 += kAtOnce) {
+        f32x2 ml[kAtOnce];
+        f32x4 v[kAtOnce][4];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float* from = base + min(p0 + k, pieces - 1) * partial_floats(D);
+            ml[k] = *reinterpret_cast<const f32x2*>(from + kManyRows * D + (wave * 32 + col) * 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[k][i] = *reinterpret_cast<const f32x4*>(from + (((wave * kBlocks + d) * 4 + i) * 64 + lane) * 4);
+        }
+        float next = top;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
+        const float f = __builtin_amdgcn_exp2f(top - next);
+        sum *= f;
+        out *= f;
+        top = next;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            if (p0 + k >= pieces) continue;
+            const float e = __builtin_amdgcn_exp2f(ml[k].x - top);
+            sum = __builtin_fmaf(e, ml[k].y, sum);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) out[i] = __builtin_fmaf(e, v[k][i / 4][i % 4], out[i]);
+        }
+    }
+    if (!r.valid) return;
+    const bool empty = !r.sees || sum == 0.f;
+    store_block<T>(a.out + (r.n * a.out_stride + (int64_t)r.head * D + 32 * d) * 2, out, empty ? 0.f : 1.f / sum, empty, half);
+    if (a.lse && half == 0 && d == 0) a.lse[(int64_t)r.n * a.heads + r.head] = empty ? kMinusInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <class T, int D>
@@ -411,33 +389,47 @@ void launch_of(const PrefillArgs& a, int grid, hipStream_t st) {
     auto* kernel = cap ? (sloped ? attn_prefill_kernel<T, D, true, true> : attn_prefill_kernel<T, D, true, false>)
                        : (sloped ? attn_prefill_kernel<T, D, false, true> : attn_prefill_kernel<T, D, false, false>);
     kernel<<<grid, kThreads, 0, st>>>(a);
+    if (a.p.n_split > 1) attn_prefill_join_kernel<T, D><<<a.p.row_tiles * a.c.kv_heads * (D / 32), kThreads, 0, st>>>(a);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
 
-constexpr int kWantedWorkgroups = 512;  // two for each unit
+constexpr int kUnits = 256;
 
 PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len) {
-    PrefillPlan p;
-    const int64_t rows = (int64_t)n_tokens * (a->heads / c->kv_heads);
+    PrefillPlan p = {};
+    const int group = a->heads / c->kv_heads;
+    const int64_t rows = (int64_t)n_tokens * group, seqs = c->n_seqs < n_tokens ? c->n_seqs : n_tokens;
+    p.few = rows <= 2 * kFewRows * seqs;
+    const int tile_rows = p.few ? kFewRows : kManyRows;
     // every sequence may leave one tile partly filled, and none has more than its rows
-    const int64_t tiles = rows / kTileRows + (c->n_seqs < n_tokens ? c->n_seqs : n_tokens), items = tiles * c->kv_heads;
-    int64_t pieces = items > kAttnTickets ? 1 : ceil_div(kWantedWorkgroups, items);
-    if (pieces > kMaxSplit) pieces = kMaxSplit;
-    if (pieces > ceil_div(max_len, 256)) pieces = ceil_div(max_len, 256);
+    const int64_t tiles = rows / tile_rows + seqs, items = tiles * c->kv_heads;
+    int64_t pieces = ceil_div(p.few ? kUnits : 2 * kUnits, items);  // (so there are tickets for all items that have pieces)
+    const int64_t most = ceil_div(max_len, p.few ? 128 : kLeastTiles * tile_of(c->dim));
+    if (pieces > (p.few ? kMaxPieces : kMaxSplit)) pieces = p.few ? kMaxPieces : kMaxSplit;
+    if (pieces > most) pieces = most;
     if (pieces < 1) pieces = 1;
     p.row_tiles = (int)tiles;
     p.n_split = (int)pieces;
+    p.n_slots = piece_slots(p.n_split);
+    // Two workgroups fit a unit.  Where all are there at once, the second half goes the other way, so that a unit has a long and a short
+    // one (causal rows); where there are more, a unit takes the next as one ends, and the longest go first.
+    const int64_t grid = items * pieces, half = ceil_div(kUnits, c->kv_heads * pieces);
+    p.fold = (int)(!p.few && grid > kUnits && grid <= 2 * kUnits && half < tiles ? half : tiles);
     p.partial_at = kAttnTicketBytes;
-    p.bytes = pieces > 1 ? p.partial_at + items * pieces * partial_floats(c->dim) * sizeof(float) : 0;
+    if (pieces > 1) {
+        p.count_at = p.partial_at + items * (p.few ? p.n_slots * ((size_t)kFewRows * c->dim + 2 * kFewRows) : pieces * partial_floats(c->dim)) * sizeof(float);
+        p.bytes = p.count_at + (p.few ? 0 : items * sizeof(int32_t));
+    }
     return p;
 }
 
 int launch_attn_prefill(const PrefillArgs& a, hipStream_t st) {
     const int64_t grid = (int64_t)a.p.row_tiles * a.p.n_split * a.c.kv_heads;
     if (grid > 0x7fffffff) return TMAN_ERR_SHAPE;
+    if (a.p.few) return launch_attn_prefill_few(a, st);
     if (a.c.type == TMAN_TYPE_F16) {
         if (a.c.dim == 64) launch_of<F16, 64>(a, (int)grid, st);
         else if (a.c.dim == 128) launch_of<F16, 128>(a, (int)grid, st);
