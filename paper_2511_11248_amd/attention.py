@@ -30,16 +30,16 @@ class _CAttn(C.Structure):
     _fields_ = [("heads", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p)]
 
 
-_types = None
+# What the checks of every call compare with, looked up once (torch is imported with the first cache, not with this module).
+_types, _int32, _float32 = {}, None, None
 
 
-def _type_of(dtype) -> int:
-    global _types
-    if _types is None:
-        import torch
+def _learn_types() -> None:
+    global _int32, _float32
+    import torch
 
-        _types = {torch.float16: TMAN_TYPE_F16, torch.bfloat16: TMAN_TYPE_BF16}
-    return _types.get(dtype, -1)
+    _types.update({torch.float16: TMAN_TYPE_F16, torch.bfloat16: TMAN_TYPE_BF16})
+    _int32, _float32 = torch.int32, torch.float32
 
 
 def _wants(ok: bool, where: str, status: int = _ERR_SHAPE) -> None:
@@ -47,8 +47,8 @@ def _wants(ok: bool, where: str, status: int = _ERR_SHAPE) -> None:
         raise TmanError(status, where)
 
 
-def _is(t, name: str) -> bool:
-    return str(t.dtype) == name and t.is_contiguous()
+def _is(t, dtype) -> bool:
+    return t.dtype is dtype and t.is_contiguous()
 
 
 _functions = None
@@ -81,10 +81,12 @@ class KvCache:
 
     def __init__(self, k_pages, v_pages, page_table):
         where = "KvCache"
+        if not _types:
+            _learn_types()
         _wants(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.is_contiguous() and v_pages.is_contiguous(), where)
-        kind = _type_of(k_pages.dtype)
+        kind = _types.get(k_pages.dtype, -1)
         _wants(kind >= 0 and v_pages.dtype == k_pages.dtype, where, _ERR_CACHE)
-        _wants(page_table.dim() == 2 and _is(page_table, "torch.int32"), where)
+        _wants(page_table.dim() == 2 and _is(page_table, _int32), where)
         self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
         n_pages, self.kv_heads, self.page, self.dim = k_pages.shape
         self.n_seqs, self.max_pages = page_table.shape
@@ -93,25 +95,32 @@ class KvCache:
                           self.page, self.dim, kind)
         self._ref = C.byref(self._c)
 
-    def _rows(self, t, where: str, heads: int = 0) -> int:
+    def _rows(self, t, where: str, heads: int, tokens: int) -> int:
         """Stride between tokens of t [tokens][heads][dim], whose heads must be contiguous."""
-        _wants(t is not None, where, _ERR_NULL)
-        shape = t.shape
-        _wants(len(shape) == 3 and shape[2] == self.dim and (not heads or shape[1] == heads), where)
-        _wants(t.dtype == self.dtype, where, _ERR_CACHE)
-        stride, head, element = t.stride()
-        _wants(element == 1 and (head == self.dim or shape[1] == 1), where)
-        return stride if shape[0] > 1 else max(stride, shape[1] * self.dim)
+        if t is None:
+            raise TmanError(_ERR_NULL, where)
+        shape, strides = t.shape, t.stride()
+        if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != self.dim:
+            raise TmanError(_ERR_SHAPE, where)
+        if t.dtype is not self.dtype:
+            raise TmanError(_ERR_CACHE, where)
+        stride, head, element = strides
+        if element != 1 or (head != self.dim and heads != 1):
+            raise TmanError(_ERR_SHAPE, where)
+        return stride if tokens > 1 else max(stride, heads * self.dim)
 
-    def _weights(self, t, where: str) -> None:
-        _wants(t is None or (t.shape == self.k_pages.shape[:3] and _is(t, "torch.float32")), where)
+    def _weights(self, t, where: str) -> int:
+        _wants(t.shape == self.k_pages.shape[:3] and _is(t, _float32), where)
+        return t.data_ptr()
 
 
 class Rope:
     """``tman_rope_t``: cos_sin fp32 [n_pos][rot / 2][2]; sections: pairs per axis of positions (None: one axis)."""
 
     def __init__(self, cos_sin, sections=None, interleaved: bool = False):
-        _wants(cos_sin.dim() == 3 and cos_sin.shape[2] == 2 and _is(cos_sin, "torch.float32"), "Rope")
+        if not _types:
+            _learn_types()
+        _wants(cos_sin.dim() == 3 and cos_sin.shape[2] == 2 and _is(cos_sin, _float32), "Rope")
         self.cos_sin = cos_sin
         pairs = cos_sin.shape[1]
         self.sections = tuple(sections) if sections is not None else (pairs,)
@@ -125,15 +134,27 @@ class Attn:
     """``tman_attn_t``: how scores are made and what a window hides; slopes fp32 [heads] on the device or None."""
 
     def __init__(self, heads: int, scale: float, cap: float = 0.0, window: int = 0, slopes=None):
-        _wants(slopes is None or (slopes.dim() == 1 and slopes.shape[0] == heads and _is(slopes, "torch.float32")), "Attn")
+        if not _types:
+            _learn_types()
+        _wants(slopes is None or (slopes.dim() == 1 and slopes.shape[0] == heads and _is(slopes, _float32)), "Attn")
         self.heads, self.scale, self.cap, self.window, self.slopes = heads, scale, cap, window, slopes
         self._c = _CAttn(heads, window, scale, cap, _ptr(slopes))
         self._ref = C.byref(self._c)
 
 
-def _ints(t, n: int, where: str, needed: bool = True) -> None:
-    _wants(t is not None or not needed, where, _ERR_NULL)
-    _wants(t is None or (t.numel() == n and _is(t, "torch.int32")), where)
+def _ints(t, n: int, where: str) -> int:
+    """Pointer to n int32 numbers."""
+    if t is None:
+        raise TmanError(_ERR_NULL, where)
+    if t.dtype is not _int32 or t.numel() != n or not t.is_contiguous():
+        raise TmanError(_ERR_SHAPE, where)
+    return t.data_ptr()
+
+
+def _floats(t, n: int, where: str) -> int:
+    if t.dtype is not _float32 or t.numel() != n or not t.is_contiguous():
+        raise TmanError(_ERR_SHAPE, where)
+    return t.data_ptr()
 
 
 def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None, weights=None,
@@ -141,24 +162,23 @@ def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, po
     """Rotates q and k (q_out may be q; both None: no queries) and writes k and v [n_tokens][kv_heads][dim] into the cache as the
     last positions of their sequences; q_start None: one token a sequence."""
     where = "tman_rope_append"
-    kv_stride = cache._rows(k, where, cache.kv_heads)
-    n = k.shape[0]
-    _wants(cache._rows(v, where, cache.kv_heads) == kv_stride and v.shape[0] == n, where)
+    _wants(k is not None, where, _ERR_NULL)
+    n, B = k.shape[0], cache.n_seqs
+    kv_stride = cache._rows(k, where, cache.kv_heads, n)
+    if cache._rows(v, where, cache.kv_heads, n) != kv_stride:
+        raise TmanError(_ERR_SHAPE, where)
     heads = q_stride = q_out_stride = 0
     if q is not None:
         heads = q.shape[1]
-        q_stride = cache._rows(q, where)
-        q_out_stride = cache._rows(q_out, where, heads)
-        _wants(q.shape[0] == n and q_out.shape[0] == n, where)
-    _ints(lens, cache.n_seqs, where)
-    _ints(q_start, cache.n_seqs + 1, where, needed=False)
-    if positions is not None:
-        _wants(rope is not None, where)
-        _ints(positions, len(rope.sections) * n, where)
-    cache._weights(weights, where)
-    _check(_load().tman_rope_append(cache._ref, rope._ref if rope is not None else None, heads, n, _ptr(q), q_stride, _ptr(k), _ptr(v),
-                                    kv_stride, _ptr(positions), _ptr(q_start), _ptr(lens), _ptr(q_out), q_out_stride,
-                                    _ptr(weights), _stream(stream)), where)
+        q_stride, q_out_stride = cache._rows(q, where, heads, n), cache._rows(q_out, where, heads, n)
+    _wants(positions is None or rope is not None, where)
+    L = _functions or _load()
+    _check(L.tman_rope_append(cache._ref, None if rope is None else rope._ref, heads, n, None if q is None else q.data_ptr(), q_stride,
+                              k.data_ptr(), v.data_ptr(), kv_stride,
+                              None if positions is None else _ints(positions, len(rope.sections) * n, where),
+                              None if q_start is None else _ints(q_start, B + 1, where), _ints(lens, B, where),
+                              None if q_out is None else q_out.data_ptr(), q_out_stride,
+                              None if weights is None else cache._weights(weights, where), _stream(stream)), where)
 
 
 def tman_attn_decode_workspace_bytes(cache: KvCache, attn: Attn, max_len: int, weights: bool = False) -> int:
@@ -169,16 +189,14 @@ def tman_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, wor
                      stream=None) -> None:
     """Attention of one new token of every sequence over its cache; the workspace is zero-filled once by the caller."""
     where = "tman_attn_decode"
-    q_stride, out_stride = cache._rows(q, where, attn.heads), cache._rows(out, where, attn.heads)
-    B = cache.n_seqs
-    _wants(q.shape[0] == B and out.shape[0] == B, where)
-    _ints(lens, B, where)
-    _ints(first, B, where, needed=False)
-    _wants(lse is None or (lse.numel() == B * attn.heads and _is(lse, "torch.float32")), where)
-    cache._weights(weights, where)
-    _check(_load().tman_attn_decode(cache._ref, attn._ref, _ptr(q), q_stride, _ptr(lens), _ptr(first), max_len, _ptr(out), out_stride,
-                                    _ptr(lse), _ptr(weights), _ptr(workspace), 0 if workspace is None else api._nbytes(workspace),
-                                    _stream(stream)), where)
+    B, H = cache.n_seqs, attn.heads
+    L = _functions or _load()
+    _check(L.tman_attn_decode(cache._ref, attn._ref, None if q is None else q.data_ptr(), cache._rows(q, where, H, B), _ints(lens, B, where),
+                              None if first is None else _ints(first, B, where), max_len, None if out is None else out.data_ptr(),
+                              cache._rows(out, where, H, B), None if lse is None else _floats(lse, B * H, where),
+                              None if weights is None else cache._weights(weights, where),
+                              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+                              _stream(stream)), where)
 
 
 def tman_attn_prefill_workspace_bytes(cache: KvCache, attn: Attn, n_tokens: int, max_len: int) -> int:
@@ -189,17 +207,15 @@ def tman_attn_prefill(cache: KvCache, attn: Attn, q, q_start, lens, out, max_len
                       stream=None) -> None:
     """Attention of the new tokens of prompts over the cache that holds them; token n sees positions first[n] <= j < end[n]."""
     where = "tman_attn_prefill"
-    q_stride, out_stride = cache._rows(q, where, attn.heads), cache._rows(out, where, attn.heads)
-    n = q.shape[0]
-    _wants(out.shape[0] == n, where)
-    _ints(q_start, cache.n_seqs + 1, where)
-    _ints(lens, cache.n_seqs, where)
-    _ints(first, n, where, needed=False)
-    _ints(end, n, where, needed=False)
-    _wants(lse is None or (lse.numel() == n * attn.heads and _is(lse, "torch.float32")), where)
-    _check(_load().tman_attn_prefill(cache._ref, attn._ref, n, _ptr(q), q_stride, _ptr(q_start), _ptr(lens), _ptr(first), _ptr(end),
-                                     max_len, _ptr(out), out_stride, _ptr(lse), _ptr(workspace),
-                                     0 if workspace is None else api._nbytes(workspace), _stream(stream)), where)
+    _wants(q is not None, where, _ERR_NULL)
+    n, B, H = q.shape[0], cache.n_seqs, attn.heads
+    L = _functions or _load()
+    _check(L.tman_attn_prefill(cache._ref, attn._ref, n, q.data_ptr(), cache._rows(q, where, H, n), _ints(q_start, B + 1, where),
+                               _ints(lens, B, where), None if first is None else _ints(first, n, where),
+                               None if end is None else _ints(end, n, where), max_len, None if out is None else out.data_ptr(),
+                               cache._rows(out, where, H, n), None if lse is None else _floats(lse, n * H, where),
+                               None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+                               _stream(stream)), where)
 
 
 def tman_kv_evict(cache: KvCache, weights, lens, keep: int, recent: int, new_table, new_lens, kept, max_len: int, stream=None) -> None:
@@ -207,10 +223,10 @@ def tman_kv_evict(cache: KvCache, weights, lens, keep: int, recent: int, new_tab
     new_table; new_lens [n_seqs] and kept [n_seqs][kv_heads][keep] receive the lengths and the positions that stayed."""
     where = "tman_kv_evict"
     _wants(weights is not None and new_table is not None, where, _ERR_NULL)
-    cache._weights(weights, where)
-    _ints(lens, cache.n_seqs, where)
-    _ints(new_lens, cache.n_seqs, where)
-    _ints(kept, cache.n_seqs * cache.kv_heads * keep, where)
-    _wants(new_table.dim() == 2 and new_table.shape[0] == cache.n_seqs and _is(new_table, "torch.int32"), where)
-    _check(_load().tman_kv_evict(cache._ref, _ptr(weights), _ptr(lens), keep, recent, max_len, _ptr(new_table), new_table.shape[1],
-                                 _ptr(new_lens), _ptr(kept), _stream(stream)), where)
+    B = cache.n_seqs
+    _wants(new_table.dim() == 2 and new_table.shape[0] == B, where)
+    pages = new_table.shape[1]
+    L = _functions or _load()
+    _check(L.tman_kv_evict(cache._ref, cache._weights(weights, where), _ints(lens, B, where), keep, recent, max_len,
+                           _ints(new_table, B * pages, where), pages, _ints(new_lens, B, where),
+                           _ints(kept, B * cache.kv_heads * keep, where), _stream(stream)), where)

@@ -22,6 +22,14 @@ constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kMaxSplit = 64;
 static_assert(kManyRows == kWaves * 32, "a wave takes 32 rows");
 constexpr float kSlack = 8.f;
+constexpr int kVector = 0x2, kMatrix = 0x8, kReadsLds = 0x100;  // kinds of instructions, for the scheduler
+#ifndef BESIDE
+#define BESIDE 4
+#define BESIDE2 3
+#define AHEAD2 8
+#define AHEAD 6
+#endif
+constexpr int kBeside = BESIDE, kBeside2 = BESIDE2;
 constexpr int kLeastTiles = 4;  // of a piece
 
 // Positions of a tile: heads of 256 leave registers for the scores of 32.
@@ -121,14 +129,18 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         const int j = t * kTile + wave * kOwnRows;
         return row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
     };
-    auto request = [&](int64_t place, uint32_t to) {
-        const u32x4 k = resource(a.c.k + place, kOwnRows * kRowBytes), v = resource(a.c.v + place, kOwnRows * kRowBytes);
+    // two buffers of keys, then two of values
+    auto request_keys = [&](int64_t place, int buffer) {
+        const u32x4 k = resource(a.c.k + place, kOwnRows * kRowBytes);
 #pragma unroll
         for (int i = 0; i < kRequests; ++i)
-            request_to_lds(k, k_ask ^ (R::key_turn(i * R::kRowsPerRequest) * 16), i * 1024, to + (wave * kRequests + i) * 1024);
+            request_to_lds(k, k_ask ^ (R::key_turn(i * R::kRowsPerRequest) * 16), i * 1024, all + buffer * kSlot + (wave * kRequests + i) * 1024);
+    };
+    auto request_values = [&](int64_t place, int buffer) {
+        const u32x4 v = resource(a.c.v + place, kOwnRows * kRowBytes);
 #pragma unroll
         for (int i = 0; i < kRequests; ++i)
-            request_to_lds(v, v_ask ^ (R::value_turn32(i * R::kRowsPerRequest) * 16), i * 1024, to + kSlot + (wave * kRequests + i) * 1024);
+            request_to_lds(v, v_ask ^ (R::value_turn32(i * R::kRowsPerRequest) * 16), i * 1024, all + (2 + buffer) * kSlot + (wave * kRequests + i) * 1024);
     };
     // reads: keys of row 32 kb + col, chunk 2 x + half; values of rows .. + 4 half, columns 32 d + 16 (lane / 16 % 2) ..
     // (turns reach the lowest 256 bytes of a row: what is further is a constant)
@@ -139,7 +151,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     const int v_row = 4 * half + ((lane & 15) >> 2);
 #pragma unroll
     for (int d = 0; d < kValueReads; ++d)
-        v_read[d] = all + kSlot + v_row * kRowBytes + (lane & 1) * 8 +
+        v_read[d] = all + 2 * kSlot + v_row * kRowBytes + (lane & 1) * 8 +
                     ((((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) ^ R::value_turn32(v_row) ^ (4 * d)) * 16;
     // kept, not made again for every tile
 #pragma unroll
@@ -156,22 +168,26 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     for (int d = 0; d < kBlocks; ++d) out[d] = f32x16{};
     float top = kLowest, sum = 0.f;
 
-    // one tile, at `buffer` of the room; PART: some query of the wave does not see all of its keys
-    auto work_on = [&](int t, uint32_t buffer, auto part) {
+    auto products = [&](uint32_t buffer, f32x16 (&s)[kKeyBlocks]) {
+        uint32_t k_at[kKeyReads];
+#pragma unroll
+        for (int x = 0; x < kKeyReads; ++x) asm("v_add_u32 %0, %1, %2" : "=v"(k_at[x]) : "s"(buffer * kSlot), "v"(k_read[x]));
+#pragma unroll
+        for (int kb = 0; kb < kKeyBlocks; ++kb) s[kb] = f32x16{};
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+            for (int kb = 0; kb < kKeyBlocks; ++kb) s[kb] = T::mfma32(lds_read<u32x4>(k_at[x & 7] + (x >> 3) * 256 + kb * 32 * kRowBytes), q[x], s[kb]);
+    };
+    // One tile, whose products are there already; those of the next one are made between its exponentials.  PART: some query of the
+    // wave does not see all of its keys.
+    auto work_on = [&](int t, f32x16 (&s)[kKeyBlocks], f32x16 (&next_s)[kKeyBlocks], auto part) {
         constexpr bool PART = decltype(part)::value;
         const int j0 = t * kTile;
-        uint32_t k_at[kKeyReads], v_at[kValueReads];
+        const uint32_t buffer = (t - t0) & 1;
+        uint32_t v_at[kValueReads];
 #pragma unroll
-        for (int x = 0; x < kKeyReads; ++x) asm("v_add_u32 %0, %1, %2" : "=v"(k_at[x]) : "s"(buffer), "v"(k_read[x]));
-#pragma unroll
-        for (int d = 0; d < kValueReads; ++d) asm("v_add_u32 %0, %1, %2" : "=v"(v_at[d]) : "s"(buffer), "v"(v_read[d]));
-        f32x16 s[kKeyBlocks];
-#pragma unroll
-        for (int kb = 0; kb < kKeyBlocks; ++kb) {
-            s[kb] = f32x16{};
-#pragma unroll
-            for (int x = 0; x < D / 16; ++x) s[kb] = T::mfma32(lds_read<u32x4>(k_at[x & 7] + (x >> 3) * 256 + kb * 32 * kRowBytes), q[x], s[kb]);
-        }
+        for (int d = 0; d < kValueReads; ++d) asm("v_add_u32 %0, %1, %2" : "=v"(v_at[d]) : "s"(buffer * kSlot), "v"(v_read[d]));
         // register i of block kb is the key at j0 + 4 half + place(kb, i)
         auto place = [](int kb, int i) { return 32 * kb + 8 * (i / 4) + i % 4; };
         float best = kMinusInf;  // the largest product or score
@@ -217,6 +233,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             for (int d = 0; d < kBlocks; ++d) out[d] *= f;
             top = next;
         }
+        if constexpr (!PART) products(buffer ^ 1, next_s);  // (behind the last tile of whatever the buffer holds; they are not used)
         u32x4 p[2 * kKeyBlocks];  // 16 keys each
         float more = 0.f;
         auto exponentials = [&](auto score) {
@@ -247,6 +264,25 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             for (int ks = 0; ks < 2 * kKeyBlocks; ++ks)
 #pragma unroll
                 for (int d = 0; d < kBlocks; ++d) out[d] = T::mfma32(values(v_at[d & 3] + (d >> 2) * 256, ks), p[ks], out[d]);
+            if constexpr (!PART) {
+                // The order of issue: reads of LDS run ahead of the products that take them, and the vector pipe has something to do
+                // beside every product.
+                constexpr int kAhead = AHEAD, kQk = kKeyBlocks * (D / 16), kPv = 2 * kKeyBlocks * kBlocks;
+                __builtin_amdgcn_sched_group_barrier(kReadsLds, kAhead, 0);
+#pragma unroll
+                for (int x = 0; x < kQk; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kReadsLds, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kVector, kBeside, 0);
+                }
+                __builtin_amdgcn_sched_group_barrier(kReadsLds, AHEAD2, 0);
+#pragma unroll
+                for (int x = 0; x < kPv; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kReadsLds, 2, 0);
+                    __builtin_amdgcn_sched_group_barrier(kVector, kBeside2, 0);
+                }
+            }
         } else {
 #pragma unroll
             for (int ks = 0; ks < 2 * kKeyBlocks; ++ks)
@@ -264,7 +300,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t chunk = (4 * d + i) ^ R::value_turn32(y);
-                        const u32x2 w = lds_read<u32x2>(all + buffer + kSlot + y * kRowBytes + chunk * 16 + half * 8);
+                        const u32x2 w = lds_read<u32x2>(all + (2 + buffer) * kSlot + y * kRowBytes + chunk * 16 + half * 8);
                         const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
                         if (seen && (m.x & 0xffffu)) out[d][4 * i] += T::low(w.x);
                         if (seen && (m.x >> 16)) out[d][4 * i + 1] += T::high(w.x);
@@ -275,40 +311,71 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         }
     };
 
-    int64_t next = 0;
+    // Keys are there a tile ahead of the values.
+    int64_t next_v = 0, next_k = 0;  // where the values of the next tile and the keys of the one behind it are
+    f32x16 s0[kKeyBlocks], s1[kKeyBlocks];
     if (t0 < t1) {
-        request(find(t0), all);
-        if (t0 + 1 < t1) next = find(t0 + 1);
+        const int64_t first = find(t0);
+        request_keys(first, 0);
+        request_values(first, 0);
+        if (t0 + 1 < t1) {
+            next_v = find(t0 + 1);
+            request_keys(next_v, 1);
+            if (t0 + 2 < t1) next_k = find(t0 + 2);
+            wait_requests<2 * kRequests>();
+        } else {
+            wait_requests<kRequests>();
+        }
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        products(0, s0);
     }
-    auto enter = [&](int t) {  // tile t is there, its buffer's neighbour is free and takes the next one
+    auto enter = [&](int t) {  // the values of tile t and the keys of the next one are there, what is behind takes their neighbours
+        const int buffer = (t - t0) & 1;
         wait_requests<0>();
         if (t * kTile < all_lo || (t + 1) * kTile > all_hi) {  // somebody compares positions: are all values finite?
             u16x2 largest = {0, 0};
 #pragma unroll
             for (int i = 0; i < kRequests; ++i)
-                largest = larger_bits(largest, lds_read<u32x4>(all + ((t - t0) & 1) * (2 * kSlot) + kSlot + (wave * kRequests + i) * 1024 + lane * 16));
+                largest = larger_bits(largest, lds_read<u32x4>(all + (2 + buffer) * kSlot + (wave * kRequests + i) * 1024 + lane * 16));
             const bool odd = __any(largest.x >= T::kExponent || largest.y >= T::kExponent);
-            if (lane == 0) odd_rows[(t - t0) & 1][wave] = odd;
+            if (lane == 0) odd_rows[buffer][wave] = odd;
         }
         wait_lds();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (t + 1 < t1) {
-            request(next, all + ((t + 1 - t0) & 1) * (2 * kSlot));
-            if (t + 2 < t1) next = find(t + 2);
+            if (t + 2 < t1) request_keys(next_k, buffer);
+            request_values(next_v, buffer ^ 1);
+            next_v = next_k;
+            if (t + 3 < t1) next_k = find(t + 3);
         }
-        return (uint32_t)((t - t0) & 1) * (2 * kSlot);
     };
     // The tiles that all queries of the wave see whole are a run; before and behind it, positions are compared.  Waves pass the
     // same number of barriers, whichever loop they are in.
     const int whole0 = min(max((inner_lo + kTile - 1) / kTile, t0), t1), whole1 = min(max(inner_hi / kTile, whole0), t1);
     int t = t0, stop = whole0;
-    while (t < t1) {
-        for (; t < stop; ++t) {
-            const uint32_t buffer = enter(t);
-            if (t * kTile < most && (t + 1) * kTile > least) work_on(t, buffer, std::true_type{});
+    auto one = [&](auto part) {
+        enter(t);
+        if constexpr (decltype(part)::value) {
+            if (t * kTile < most && (t + 1) * kTile > least) work_on(t, s0, s0, part);
+            products(((t - t0) & 1) ^ 1, s0);
+        } else {
+            work_on(t, s0, s1, part);
+#pragma unroll
+            for (int kb = 0; kb < kKeyBlocks; ++kb) s0[kb] = s1[kb];
         }
-        for (; t < whole1; ++t) work_on(t, enter(t), std::false_type{});
+        ++t;
+    };
+    while (t < t1) {
+        while (t < stop) one(std::true_type{});
+        for (; t + 1 < whole1; t += 2) {  // (two at a time: what is next need not be moved)
+            enter(t);
+            work_on(t, s0, s1, std::false_type{});
+            enter(t + 1);
+            work_on(t + 1, s1, s0, std::false_type{});
+        }
+        if (t < whole1) one(std::false_type{});
         stop = t1;
     }
     sum = sum_halves(sum);
@@ -404,8 +471,8 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     const int64_t rows = (int64_t)n_tokens * group, seqs = c->n_seqs < n_tokens ? c->n_seqs : n_tokens;
     p.few = rows <= 2 * kFewRows * seqs;
     const int tile_rows = p.few ? kFewRows : kManyRows;
-    // every sequence may leave one tile partly filled, and none has more than its rows
-    const int64_t tiles = rows / tile_rows + seqs, items = tiles * c->kv_heads;
+    // each sequence may leave one tile filled with a single row
+    const int64_t tiles = (rows + seqs * (tile_rows - 1)) / tile_rows, items = tiles * c->kv_heads;
     int64_t pieces = ceil_div(p.few ? kUnits : 2 * kUnits, items);  // (so there are tickets for all items that have pieces)
     const int64_t most = ceil_div(max_len, p.few ? 128 : kLeastTiles * tile_of(c->dim));
     if (pieces > (p.few ? kMaxPieces : kMaxSplit)) pieces = p.few ? kMaxPieces : kMaxSplit;
