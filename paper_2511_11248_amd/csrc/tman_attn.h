@@ -52,10 +52,11 @@ int launch_attn_decode(const DecodeArgs& a, hipStream_t st);
 
 // A prefill launch: a workgroup takes some rows - the new tokens of one sequence times the query heads of one key-value head - and
 // one piece of the positions.  Few rows go to a kernel whose waves share out the positions (32 rows a workgroup, pieces meet as in
-// decoding), many to one whose waves share out the rows (128, pieces meet in a second kernel).
+// decoding, or in a second kernel), many to one whose waves share out the rows (128, pieces meet in a second kernel).
 constexpr int kFewRows = 32, kManyRows = 128;
 struct PrefillPlan {
     int few;
+    int second;     // pieces meet in a second kernel
     int row_tiles;  // at most, over all sequences
     int n_split;    // pieces, at most
     int n_slots;    // of partial sums for an item (few)
@@ -77,7 +78,7 @@ struct PrefillArgs {
     int64_t q_stride, out_stride;
     int32_t* tickets;
     float* partial;
-    int32_t* counts;  // pieces of every item (many rows)
+    int32_t* counts;  // pieces of every item, for the second kernel
     float scale, cap;
     int heads, group, window, max_len, n_tokens;
     PrefillPlan p;

@@ -95,13 +95,15 @@ __device__ __forceinline__ void report_index_error(int* status) {
     __hip_atomic_store(status, (int)TMAN_ERR_INDEX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Length of sequence b, cut to what its table and the caller's bound hold.
-__device__ __forceinline__ int checked_length(const KvView& c, const int32_t* lens, int b, int max_len) {
-    const int n = scalar_load(lens, b);
+// A sequence's length, cut to what its table and the caller's bound hold.
+__device__ __forceinline__ int checked_length(const KvView& c, int n, int max_len) {
     const int most = min(max_len, c.max_pages << c.page_shift);
     if ((unsigned)n <= (unsigned)most) return n;
     report_index_error(c.status);
     return n < 0 ? 0 : most;
+}
+__device__ __forceinline__ int checked_length(const KvView& c, const int32_t* lens, int b, int max_len) {
+    return checked_length(c, scalar_load(lens, b), max_len);
 }
 // Pool index of entry `i` of sequence b's table, cut to the pool; one that is `used` and outside is reported.
 __device__ __forceinline__ int checked_page(const KvView& c, int b, int i, bool used) {
@@ -178,15 +180,19 @@ struct RowTile {
     int b;       // sequence, -1: there is no such tile
     int tile;    // of the sequence
     int start, tokens;
+    int len;
 };
 template <int ROWS>
 __device__ __forceinline__ RowTile find_row_tile(const PrefillArgs& a, int item, int lane) {
-    RowTile r = {-1, item, 0, 0};
+    RowTile r = {-1, item, 0, 0, 0};
     for (int at = 0; at < a.c.n_seqs; at += 64) {
-        int s0 = 0, n = 0;
+        int s0 = 0, n = 0, len = 0;
         if (at + lane < a.c.n_seqs) {
-            s0 = min(max(a.q_start[at + lane], 0), a.n_tokens);
-            n = min(max(a.q_start[at + lane + 1], s0), a.n_tokens) - s0;
+            s0 = a.q_start[at + lane];
+            n = a.q_start[at + lane + 1];
+            len = a.lens[at + lane];
+            s0 = min(max(s0, 0), a.n_tokens);
+            n = min(max(n, s0), a.n_tokens) - s0;
         }
         const int tiles = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
         int run = tiles;
@@ -204,6 +210,8 @@ __device__ __forceinline__ RowTile find_row_tile(const PrefillArgs& a, int item,
             r.tile -= __builtin_amdgcn_readlane(run - tiles, l);
             r.start = __builtin_amdgcn_readlane(s0, l);
             r.tokens = __builtin_amdgcn_readlane(n, l);
+            r.len = checked_length(a.c, __builtin_amdgcn_readlane(len, l), a.max_len);
+            if (r.tokens > r.len && threadIdx.x == 0) report_index_error(a.c.status);
             return r;
         }
         r.tile -= __builtin_amdgcn_readlane(run, 63);

@@ -67,47 +67,56 @@ struct Join {
         return *last != 0;
     }
 
-    // Adds up `count` slots from `first`, in their order.  A thread takes four coordinates of a column and every `shares`-th slot, with the
-    // reads of several under way at once; the shares then meet in LDS (at `room`, 24 bytes a thread).
+    // Four coordinates d .. of column c of every `shares`-th of `count` slots from number `share` on, in their order, the reads of several
+    // under way at once.
+    template <class F>
+    static __device__ __forceinline__ void quad(const float* first, int count, int share, int shares, int c, int d, F done) {
+        float m = kLowest, l = 0.f;
+        f32x4 o = {0, 0, 0, 0};
+        for (int p0 = share; p0 < count; p0 += kAtOnce * shares) {
+            f32x2 ml[kAtOnce], v[kAtOnce][2];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const float* from = first + min(p0 + k * shares, count - 1) * kSlotFloats;
+                ml[k] = load_shared(from + COLS * D + 2 * c);
+                v[k][0] = load_shared(from + c * D + d);
+                v[k][1] = load_shared(from + c * D + d + 2);
+            }
+            float next = m;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
+            const float f = __builtin_amdgcn_exp2f(m - next);
+            l *= f;
+            o *= f;
+            m = next;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                if (p0 + k * shares >= count) continue;
+                const float e = __builtin_amdgcn_exp2f(ml[k].x - m);
+                l = __builtin_fmaf(e, ml[k].y, l);
+                o += e * f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y};
+            }
+        }
+        done(c, d, m, l, o);
+    }
+
+    // Adds up `count` slots from `first`.  A thread takes four coordinates of a column and every `shares`-th slot; the shares then meet in
+    // LDS (at `room`, 24 bytes a thread).
     template <class F>
     static __device__ __forceinline__ void slots(const float* first, int count, int n_cols, uint32_t room, F done) {
         const int quads = n_cols * (D / 4);
         int shares = 1;
         while (shares * 2 * quads <= kThreads && shares * kAtOnce < count) shares *= 2;
         for (int x = threadIdx.x; x < quads * shares; x += kThreads) {
-            const int share = x / quads, y = x - share * quads, c = y / (D / 4), d = y % (D / 4) * 4;
-            float m = kLowest, l = 0.f;
-            f32x4 o = {0, 0, 0, 0};
-            for (int p0 = share; p0 < count; p0 += kAtOnce * shares) {
-                f32x2 ml[kAtOnce], v[kAtOnce][2];
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const float* from = first + min(p0 + k * shares, count - 1) * kSlotFloats;
-                    ml[k] = load_shared(from + COLS * D + 2 * c);
-                    v[k][0] = load_shared(from + c * D + d);
-                    v[k][1] = load_shared(from + c * D + d + 2);
+            const int share = x / quads, y = x - share * quads;
+            quad(first, count, share, shares, y / (D / 4), y % (D / 4) * 4, [&](int c, int d, float m, float l, f32x4 o) {
+                if (shares > 1) {
+                    lds_write(room + x * 16, o);
+                    lds_write(room + kThreads * 16 + x * 8, f32x2{m, l});
+                } else {
+                    done(c, d, m, l, o);
                 }
-                float next = m;
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) next = fmaxf(next, ml[k].x);
-                const float f = __builtin_amdgcn_exp2f(m - next);
-                l *= f;
-                o *= f;
-                m = next;
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    if (p0 + k * shares >= count) continue;
-                    const float e = __builtin_amdgcn_exp2f(ml[k].x - m);
-                    l = __builtin_fmaf(e, ml[k].y, l);
-                    o += e * f32x4{v[k][0].x, v[k][0].y, v[k][1].x, v[k][1].y};
-                }
-            }
-            if (shares > 1) {
-                lds_write(room + x * 16, o);
-                lds_write(room + kThreads * 16 + x * 8, f32x2{m, l});
-            } else {
-                done(c, d, m, l, o);
-            }
+            });
         }
         if (shares == 1) return;
         __syncthreads();

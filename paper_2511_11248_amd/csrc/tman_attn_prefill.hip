@@ -30,10 +30,14 @@ constexpr int kVector = 0x2, kMatrix = 0x8, kReadsLds = 0x100;  // kinds of inst
 #define AHEAD 6
 #endif
 constexpr int kBeside = BESIDE, kBeside2 = BESIDE2;
-constexpr int kLeastTiles = 4;  // of a piece
+constexpr int kLeastTiles = 8;  // of a piece
 
 // Positions of a tile: heads of 256 leave registers for the scores of 32.
 __host__ __device__ constexpr int tile_of(int D) { return D == 256 ? 32 : 64; }
+
+// Buffers of tiles in LDS, so how far ahead requests go out: what fits two workgroups a unit (heads of 256: one, whose registers leave no
+// room for a second).
+__host__ __device__ constexpr int buffers_of(int D) { return D == 128 ? 2 : 4; }
 
 // [item][piece]: every wave's accumulators as they lie in its lanes, then the maxima and sums of its columns
 __host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kManyRows * D + 2 * kManyRows; }
@@ -60,9 +64,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     constexpr int kOwnRows = kTile / kWaves;                            // rows that a wave requests of a tile: 8 or 16, in one page
     constexpr int kRequests = kOwnRows * kRowBytes / 1024;              // and as many requests for the values
     constexpr int kBlocks = D / 32;
-    __shared__ __attribute__((aligned(1024))) uint8_t room[2 * 2 * kSlot];
+    constexpr int kBuffers = buffers_of(D), kAheadRequests = (kBuffers - 2) * 2 * kRequests;
+    __shared__ __attribute__((aligned(1024))) uint8_t room[kBuffers * 2 * kSlot];
     __shared__ Span wave_span[kWaves];
-    __shared__ __attribute__((aligned(16))) uint32_t odd_rows[2][kWaves];  // of a buffer's values: those that a wave requested are not all finite
+    __shared__ __attribute__((aligned(16))) uint32_t odd_rows[kBuffers][kWaves];  // of a buffer's values: those that a wave requested are not all finite
 
     const int wave = scalar((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int col = lane & 31, half = lane >> 5;
@@ -75,8 +80,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         if (a.p.n_split > 1 && piece == 0 && threadIdx.x == 0) a.counts[(int64_t)item * a.c.kv_heads + hk] = 0;
         return;
     }
-    const int b = rows.b, len = checked_length(a.c, a.lens, b, a.max_len);
-    if (rows.tokens > len && threadIdx.x == 0) report_index_error(a.c.status);
+    const int b = rows.b, len = rows.len;
     const int64_t row0 = (int64_t)rows.tile * kManyRows;
     const QueryRow r = query_row(a, rows, row0 + wave * 32 + col, hk, len);
     const int at = r.at, lo = r.lo, hi = r.hi, n = r.n, head = r.head;
@@ -102,7 +106,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     const int all_lo = scalar(whole.inner_lo), all_hi = scalar(whole.inner_hi);  // all rows see whole tiles between them
     const int least = scalar(span.least), most = scalar(span.most), inner_lo = scalar(span.inner_lo), inner_hi = scalar(span.inner_hi);
     const int least_at = scalar(span.least_at);
-    const int per_piece = max((n_tiles + a.p.n_split - 1) / a.p.n_split, kLeastTiles);
+    const int per_piece = max((n_tiles + a.p.n_split - 1) / a.p.n_split, kLeastTiles * 64 / kTile);
     const int pieces = max((n_tiles + per_piece - 1) / per_piece, 1);
     if (a.p.n_split > 1 && piece == 0 && threadIdx.x == 0) a.counts[(int64_t)item * a.c.kv_heads + hk] = pieces;
     if (piece >= pieces) return;
@@ -129,7 +133,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         const int j = t * kTile + wave * kOwnRows;
         return row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
     };
-    // two buffers of keys, then two of values
+    // the buffers of keys, then those of values
     auto request_keys = [&](int64_t place, int buffer) {
         const u32x4 k = resource(a.c.k + place, kOwnRows * kRowBytes);
 #pragma unroll
@@ -140,7 +144,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         const u32x4 v = resource(a.c.v + place, kOwnRows * kRowBytes);
 #pragma unroll
         for (int i = 0; i < kRequests; ++i)
-            request_to_lds(v, v_ask ^ (R::value_turn32(i * R::kRowsPerRequest) * 16), i * 1024, all + (2 + buffer) * kSlot + (wave * kRequests + i) * 1024);
+            request_to_lds(v, v_ask ^ (R::value_turn32(i * R::kRowsPerRequest) * 16), i * 1024, all + (kBuffers + buffer) * kSlot + (wave * kRequests + i) * 1024);
     };
     // reads: keys of row 32 kb + col, chunk 2 x + half; values of rows .. + 4 half, columns 32 d + 16 (lane / 16 % 2) ..
     // (turns reach the lowest 256 bytes of a row: what is further is a constant)
@@ -151,7 +155,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     const int v_row = 4 * half + ((lane & 15) >> 2);
 #pragma unroll
     for (int d = 0; d < kValueReads; ++d)
-        v_read[d] = all + 2 * kSlot + v_row * kRowBytes + (lane & 1) * 8 +
+        v_read[d] = all + kBuffers * kSlot + v_row * kRowBytes + (lane & 1) * 8 +
                     ((((lane >> 4) & 1) * 2 + ((lane >> 1) & 1)) ^ R::value_turn32(v_row) ^ (4 * d)) * 16;
     // kept, not made again for every tile
 #pragma unroll
@@ -184,7 +188,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     auto work_on = [&](int t, f32x16 (&s)[kKeyBlocks], f32x16 (&next_s)[kKeyBlocks], auto part) {
         constexpr bool PART = decltype(part)::value;
         const int j0 = t * kTile;
-        const uint32_t buffer = (t - t0) & 1;
+        const uint32_t buffer = (t - t0) % kBuffers;
         uint32_t v_at[kValueReads];
 #pragma unroll
         for (int d = 0; d < kValueReads; ++d) asm("v_add_u32 %0, %1, %2" : "=v"(v_at[d]) : "s"(buffer * kSlot), "v"(v_read[d]));
@@ -233,7 +237,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             for (int d = 0; d < kBlocks; ++d) out[d] *= f;
             top = next;
         }
-        if constexpr (!PART) products(buffer ^ 1, next_s);  // (behind the last tile of whatever the buffer holds; they are not used)
+        if constexpr (!PART) products((buffer + 1) % kBuffers, next_s);  // (behind the last tile of whatever the buffer holds; they are not used)
         u32x4 p[2 * kKeyBlocks];  // 16 keys each
         float more = 0.f;
         auto exponentials = [&](auto score) {
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         sum += more;
         bool odd_values = false;
         if constexpr (PART) {
-            const u32x4 f = *reinterpret_cast<const u32x4*>(odd_rows[(t - t0) & 1]);
+            const u32x4 f = *reinterpret_cast<const u32x4*>(odd_rows[buffer]);
             odd_values = scalar((int)(f.x | f.y | f.z | f.w)) != 0;
         }
         if (!PART || !odd_values) {
@@ -300,7 +304,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t chunk = (4 * d + i) ^ R::value_turn32(y);
-                        const u32x2 w = lds_read<u32x2>(all + (2 + buffer) * kSlot + y * kRowBytes + chunk * 16 + half * 8);
+                        const u32x2 w = lds_read<u32x2>(all + (kBuffers + buffer) * kSlot + y * kRowBytes + chunk * 16 + half * 8);
                         const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
                         if (seen && (m.x & 0xffffu)) out[d][4 * i] += T::low(w.x);
                         if (seen && (m.x >> 16)) out[d][4 * i + 1] += T::high(w.x);
@@ -311,45 +315,43 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         }
     };
 
-    // Keys are there a tile ahead of the values.
-    int64_t next_v = 0, next_k = 0;  // where the values of the next tile and the keys of the one behind it are
+    // Step t requests the keys of tile t + kBuffers and the values of tile t + kBuffers - 1, in this order (also ahead of the first tile):
+    // the keys of tile t and the values of tile t - 1 have been read by all waves then.
+    int64_t next = 0, last = 0;  // where the tile of the next step's keys and the one before it are
+    auto step = [&](int i) {
+        if (i + kBuffers < t1) request_keys(next, (i - t0 + kBuffers) % kBuffers);
+        if (i + kBuffers - 1 >= t0 && i + kBuffers - 1 < t1) request_values(last, (i - t0 + 2 * kBuffers - 1) % kBuffers);
+        last = next;
+        if (i + 1 + kBuffers < t1) next = find(i + 1 + kBuffers);
+    };
     f32x16 s0[kKeyBlocks], s1[kKeyBlocks];
     if (t0 < t1) {
-        const int64_t first = find(t0);
-        request_keys(first, 0);
-        request_values(first, 0);
-        if (t0 + 1 < t1) {
-            next_v = find(t0 + 1);
-            request_keys(next_v, 1);
-            if (t0 + 2 < t1) next_k = find(t0 + 2);
-            wait_requests<2 * kRequests>();
-        } else {
-            wait_requests<kRequests>();
-        }
+        next = find(t0);
+#pragma unroll
+        for (int i = -kBuffers; i < 0; ++i) step(t0 + i);
+        // the first keys: all requests of the steps behind theirs may be under way, where there are that many
+        if (t0 + kBuffers <= t1) wait_requests<kAheadRequests + 2 * kRequests>();
+        else wait_requests<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         products(0, s0);
     }
-    auto enter = [&](int t) {  // the values of tile t and the keys of the next one are there, what is behind takes their neighbours
-        const int buffer = (t - t0) & 1;
-        wait_requests<0>();
+    auto enter = [&](int t) {  // the values of tile t and the keys of the next one are there
+        const int buffer = (t - t0) % kBuffers;
+        if (t + kBuffers <= t1) wait_requests<kAheadRequests>();  // (the last kBuffers - 2 steps asked for all they could)
+        else wait_requests<0>();
         if (t * kTile < all_lo || (t + 1) * kTile > all_hi) {  // somebody compares positions: are all values finite?
             u16x2 largest = {0, 0};
 #pragma unroll
             for (int i = 0; i < kRequests; ++i)
-                largest = larger_bits(largest, lds_read<u32x4>(all + (2 + buffer) * kSlot + (wave * kRequests + i) * 1024 + lane * 16));
+                largest = larger_bits(largest, lds_read<u32x4>(all + (kBuffers + buffer) * kSlot + (wave * kRequests + i) * 1024 + lane * 16));
             const bool odd = __any(largest.x >= T::kExponent || largest.y >= T::kExponent);
             if (lane == 0) odd_rows[buffer][wave] = odd;
         }
         wait_lds();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (t + 1 < t1) {
-            if (t + 2 < t1) request_keys(next_k, buffer);
-            request_values(next_v, buffer ^ 1);
-            next_v = next_k;
-            if (t + 3 < t1) next_k = find(t + 3);
-        }
+        step(t);
     };
     // The tiles that all queries of the wave see whole are a run; before and behind it, positions are compared.  Waves pass the
     // same number of barriers, whichever loop they are in.
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         enter(t);
         if constexpr (decltype(part)::value) {
             if (t * kTile < most && (t + 1) * kTile > least) work_on(t, s0, s0, part);
-            products(((t - t0) & 1) ^ 1, s0);
+            products((uint32_t)(t + 1 - t0) % kBuffers, s0);
         } else {
             work_on(t, s0, s1, part);
 #pragma unroll
@@ -412,8 +414,7 @@ __global__ __launch_bounds__(kThreads) void attn_prefill_join_kernel(PrefillArgs
     if (pieces <= 1) return;
     const RowTile rows = find_row_tile<kManyRows>(a, item, lane);
     if (rows.b < 0) return;
-    const int len = checked_length(a.c, a.lens, rows.b, a.max_len);
-    const QueryRow r = query_row(a, rows, (int64_t)rows.tile * kManyRows + wave * 32 + col, hk, len);
+    const QueryRow r = query_row(a, rows, (int64_t)rows.tile * kManyRows + wave * 32 + col, hk, rows.len);
     if (!__any(r.valid)) return;
     const float* base = a.partial + at * a.p.n_split * partial_floats(D);
     float top = kLowest, sum = 0.f;
@@ -464,23 +465,32 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 }  // namespace
 
 constexpr int kUnits = 256;
+constexpr int kShort = 2048;
+constexpr int kFewJoined = 8;  // rows a sequence that the last workgroup to arrive adds up as fast as a second kernel
 
 PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len) {
     PrefillPlan p = {};
     const int group = a->heads / c->kv_heads;
     const int64_t rows = (int64_t)n_tokens * group, seqs = c->n_seqs < n_tokens ? c->n_seqs : n_tokens;
-    p.few = rows <= 2 * kFewRows * seqs;
+    // The kernel for few rows reads the keys once for every 32 rows, but starts and ends sooner and fills the chip with fewer rows: it
+    // takes up to 128 rows a sequence (32 heads over 8, 32 tokens at 4096: 16 us, the other 22; 40 tokens at 16384: both 41), and short
+    // sequences as long as three workgroups a unit will do (256 tokens 8.9 and 12.5 us, 512 tokens 13 and 18, 1000 tokens of 4 heads 16
+    // and 25; 100 tokens at 4096 30 and 27, 200 at 16384 109 and 80).
+    p.few = rows <= 4 * kFewRows * seqs || (max_len <= kShort && (rows + seqs * (kFewRows - 1)) / kFewRows * c->kv_heads <= 3 * kUnits);
     const int tile_rows = p.few ? kFewRows : kManyRows;
     // each sequence may leave one tile filled with a single row
     const int64_t tiles = (rows + seqs * (tile_rows - 1)) / tile_rows, items = tiles * c->kv_heads;
-    int64_t pieces = ceil_div(p.few ? kUnits : 2 * kUnits, items);  // (so there are tickets for all items that have pieces)
-    const int64_t most = ceil_div(max_len, p.few ? 128 : kLeastTiles * tile_of(c->dim));
+    // Few rows: a workgroup for every unit.  Many: what two workgroups a unit hold at once, and pieces of kLeastTiles tiles of what a
+    // token sees in the middle of a causal prompt.
+    int64_t pieces = p.few ? ceil_div(kUnits, items) : 2 * kUnits / items;  // (so there are tickets for all items that have pieces)
+    const int64_t seen = max_len - n_tokens / seqs / 2, most = ceil_div(p.few ? max_len : seen, p.few ? 256 : kLeastTiles * 64);
     if (pieces > (p.few ? kMaxPieces : kMaxSplit)) pieces = p.few ? kMaxPieces : kMaxSplit;
     if (pieces > most) pieces = most;
     if (pieces < 1) pieces = 1;
     p.row_tiles = (int)tiles;
     p.n_split = (int)pieces;
     p.n_slots = piece_slots(p.n_split);
+    p.second = pieces > 1 && (!p.few || rows > kFewJoined * seqs);
     // Two workgroups fit a unit.  Where all are there at once, the second half goes the other way, so that a unit has a long and a short
     // one (causal rows); where there are more, a unit takes the next as one ends, and the longest go first.
     const int64_t grid = items * pieces, half = ceil_div(kUnits, c->kv_heads * pieces);
@@ -488,7 +498,7 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     p.partial_at = kAttnTicketBytes;
     if (pieces > 1) {
         p.count_at = p.partial_at + items * (p.few ? p.n_slots * ((size_t)kFewRows * c->dim + 2 * kFewRows) : pieces * partial_floats(c->dim)) * sizeof(float);
-        p.bytes = p.count_at + (p.few ? 0 : items * sizeof(int32_t));
+        p.bytes = p.count_at + (p.second ? items * sizeof(int32_t) : 0);
     }
     return p;
 }

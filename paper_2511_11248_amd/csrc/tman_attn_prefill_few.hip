@@ -12,6 +12,24 @@ namespace {
 constexpr int kTile = 32;  // positions a wave takes at once
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 
+__device__ __forceinline__ int columns_of(const PrefillArgs& a, const RowTile& t) {  // rows of a tile
+    const int64_t n = (int64_t)t.tokens * a.group - (int64_t)t.tile * kFewRows;
+    return n < kFewRows ? (int)n : kFewRows;
+}
+
+// Four coordinates of row c of a tile, from their sums relative to the maximum m and the sum l of probabilities.
+template <class T, int D>
+__device__ __forceinline__ void store_row(const PrefillArgs& a, const RowTile& t, int hk, int c, int d, float m, float l, f32x4 o) {
+    const int row = t.tile * kFewRows + c, token = row / a.group, head = hk * a.group + row - token * a.group;
+    const int64_t n = t.start + token;
+    const bool empty = l == 0.f;  // nothing seen, or nothing of any weight
+    const float inv = empty ? 0.f : 1.f / l;
+    u32x2 w = {T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
+    if (empty) w = u32x2{0, 0};
+    *reinterpret_cast<u32x2*>(a.out + (n * a.out_stride + (int64_t)head * D + d) * 2) = w;
+    if (d == 0 && a.lse) a.lse[n * a.heads + head] = empty ? kMinusInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 template <class T, int D, bool CAP>
 __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_kernel(PrefillArgs a) {
     using R = RowsOf<D>;
@@ -28,9 +46,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
     const int hk = (int)blockIdx.x % a.c.kv_heads, rest = (int)blockIdx.x / a.c.kv_heads;
     const int piece = rest % a.p.n_split, item = a.p.row_tiles - 1 - rest / a.p.n_split;
     const RowTile rows = find_row_tile<kFewRows>(a, item, lane);
-    if (rows.b < 0) return;
-    const int b = rows.b, len = checked_length(a.c, a.lens, b, a.max_len);
-    if (rows.tokens > len && threadIdx.x == 0) report_index_error(a.c.status);
+    const int64_t at = (int64_t)item * a.c.kv_heads + hk;
+    if (rows.b < 0) {
+        if (a.p.second && piece == 0 && threadIdx.x == 0) a.counts[at] = 0;
+        return;
+    }
+    const int b = rows.b, len = rows.len;
     const int64_t row0 = (int64_t)rows.tile * kFewRows;
     const QueryRow r = query_row(a, rows, row0 + col, hk, len);
     const Span s = a.first || a.end ? span_of_columns(r) : span_of_rows(a, rows, row0, kFewRows, len);
@@ -38,6 +59,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
     const int first_tile = least < most ? least / kTile : 0, n_tiles = least < most ? (most + kTile - 1) / kTile - first_tile : 0;
     const int per_piece = max((n_tiles + a.p.n_split - 1) / a.p.n_split, kWaves);
     const int pieces = max((n_tiles + per_piece - 1) / per_piece, 1);
+    if (a.p.second && piece == 0 && threadIdx.x == 0) a.counts[at] = pieces;
     if (piece >= pieces) return;
     const int t0 = first_tile + piece * per_piece, t1 = min(first_tile + n_tiles, t0 + per_piece);
 
@@ -194,34 +216,43 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
             lds_write(mine + (col * Meet::kStride + 32 * d + 8 * i + 4 * half) * 4, f32x4{out[d][4 * i], out[d][4 * i + 1], out[d][4 * i + 2], out[d][4 * i + 3]});
     __syncthreads();
 
-    const int64_t n_rows = (int64_t)rows.tokens * a.group - row0;
-    const int n_cols = n_rows < kFewRows ? (int)n_rows : kFewRows;
-    auto finish = [&](int c, int d, float m, float l, f32x4 o) {
-        const int token = ((int)row0 + c) / a.group, head = hk * a.group + (int)row0 + c - token * a.group;
-        const int64_t n = rows.start + token;
-        const bool empty = l == 0.f;  // nothing seen, or nothing of any weight
-        const float inv = empty ? 0.f : 1.f / l;
-        u32x2 w = {T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv)};
-        if (empty) w = u32x2{0, 0};
-        *reinterpret_cast<u32x2*>(a.out + (n * a.out_stride + (int64_t)head * D + d) * 2) = w;
-        if (d == 0 && a.lse) a.lse[n * a.heads + head] = empty ? kMinusInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
-    };
+    const int n_cols = columns_of(a, rows);
+    auto finish = [&](int c, int d, float m, float l, f32x4 o) { store_row<T, D>(a, rows, hk, c, d, m, l, o); };
     if (pieces == 1) {
         Meet::waves(all, kWaveBytes, wave_max, wave_sum, n_cols, finish);
         return;
     }
-    const int64_t at = (int64_t)item * a.c.kv_heads + hk;
     float* base = a.partial + at * a.p.n_slots * Meet::kSlotFloats;
     Meet::waves(all, kWaveBytes, wave_max, wave_sum, n_cols, [&](int c, int d, float m, float l, f32x4 o) {
         Meet::publish(base + piece * Meet::kSlotFloats, c, d, m, l, o);
     });
+    if (a.p.second) return;
     Meet::pieces(base, a.tickets + at * (1 + a.p.n_slots - a.p.n_split), piece, pieces, a.p.n_split, n_cols, all, &last, finish);
+}
+
+// The pieces of an item's rows, where they are too many for one workgroup: a thread takes four coordinates of a row.
+template <class T, int D>
+__global__ __launch_bounds__(kThreads) void attn_prefill_few_join_kernel(PrefillArgs a) {
+    using Meet = Join<D, kFewRows, kWaves>;
+    constexpr int kParts = kFewRows * (D / 4) / kThreads;
+    const int part = (int)blockIdx.x % kParts, rest = (int)blockIdx.x / kParts, hk = rest % a.c.kv_heads, item = rest / a.c.kv_heads;
+    const int64_t at = (int64_t)item * a.c.kv_heads + hk;
+    const int pieces = scalar_load(a.counts, at);
+    if (pieces <= 1) return;
+    const RowTile rows = find_row_tile<kFewRows>(a, item, threadIdx.x & 63);
+    if (rows.b < 0) return;
+    const int x = part * kThreads + threadIdx.x, c = x / (D / 4), d = x % (D / 4) * 4;
+    if (c >= columns_of(a, rows)) return;
+    Meet::quad(a.partial + at * a.p.n_slots * Meet::kSlotFloats, pieces, 0, 1, c, d,
+               [&](int c, int d, float m, float l, f32x4 o) { store_row<T, D>(a, rows, hk, c, d, m, l, o); });
 }
 
 template <class T, int D>
 void launch_of(const PrefillArgs& a, int grid, hipStream_t st) {
     auto* kernel = a.cap > 0.f ? attn_prefill_few_kernel<T, D, true> : attn_prefill_few_kernel<T, D, false>;
     kernel<<<grid, kThreads, 0, st>>>(a);
+    if (a.p.second)
+        attn_prefill_few_join_kernel<T, D><<<a.p.row_tiles * a.c.kv_heads * (kFewRows * (D / 4) / kThreads), kThreads, 0, st>>>(a);
 }
 
 }  // namespace
