@@ -246,10 +246,17 @@ __device__ __forceinline__ QueryRow query_row(const PrefillArgs& a, const RowTil
 struct Span {
     int least, most, inner_lo, inner_hi, least_at;
 };
+template <int CTRL>
+__device__ __forceinline__ int min_across(int x) {  // with the lane that the cross-lane pattern CTRL names
+    return min(x, __builtin_amdgcn_update_dpp(x, x, CTRL, 0xf, 0xf, false));
+}
 __device__ __forceinline__ int min_of_columns(int x) {
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) x = min(x, __shfl_xor(x, d));
-    return scalar(x);
+    x = min_across<0xb1>(x);   // neighbours in pairs,
+    x = min_across<0x4e>(x);   // pairs in fours,
+    x = min_across<0x141>(x);  // fours in eights,
+    x = min_across<0x140>(x);  // eights in rows of 16,
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);  // rows in halves
+    return scalar(min((int)r[0], (int)r[1]));
 }
 constexpr int kNoPosition = 0x7fffffff;
 __device__ __forceinline__ Span span_of_columns(const QueryRow& r) {  // of the wave's 32 columns
@@ -272,6 +279,18 @@ __device__ __forceinline__ Span span_of_rows(const PrefillArgs& a, const RowTile
     s.inner_hi = first + 1;
     s.least_at = first;
     return s;
+}
+
+// Which of 32 positions from j on lie in [lo, hi), a bit each, less the first `skip`.
+__device__ __forceinline__ uint32_t seen_bits(int j, int lo, int hi, int skip) {
+    const int l = min(max(lo - j, 0), 32), h = min(max(hi - j, 0), 32);
+    const uint64_t below_hi = (1ull << h) - 1, below_lo = (1ull << l) - 1;
+    return (uint32_t)(below_hi & ~below_lo) >> skip;
+}
+// x where bit b is set, else minus infinity: two operations
+__device__ __forceinline__ float if_seen(float x, uint32_t bits, int b) {
+    const uint32_t all = (uint32_t)((int32_t)(bits << (31 - b)) >> 31);
+    return __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, x) & all) | (~all & 0xff800000u));
 }
 
 // the elements of w that are not finite, as all ones

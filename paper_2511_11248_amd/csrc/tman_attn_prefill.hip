@@ -209,17 +209,19 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
                 }
             best -= bias;
         } else if (PART || SLOPED) {
+            const float distance = (float)(at - j0 - 4 * half);
 #pragma unroll
-            for (int kb = 0; kb < kKeyBlocks; ++kb)
+            for (int kb = 0; kb < kKeyBlocks; ++kb) {
+                const uint32_t seen = PART ? seen_bits(j0 + 32 * kb, lo, hi, 4 * half) : 0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const int j = j0 + 4 * half + place(kb, i);
                     float x = score_of<CAP>(s[kb][i], rule);
-                    if constexpr (SLOPED) x = __builtin_fmaf(-slope, fabsf((float)(at - j)), x);
-                    if constexpr (PART) x = j >= lo && j < hi ? x : kMinusInf;
+                    if constexpr (SLOPED) x = __builtin_fmaf(-slope, fabsf(distance - (float)place(kb, i)), x);
+                    if constexpr (PART) x = if_seen(x, seen, place(0, i));
                     s[kb][i] = x;
                     best = fmaxf(best, x);
                 }
+            }
         } else {
 #pragma unroll
             for (int kb = 0; kb < kKeyBlocks; ++kb)

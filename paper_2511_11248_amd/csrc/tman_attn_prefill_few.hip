@@ -129,16 +129,15 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
         wait_lds();  // the keys have been read
         if (more) request(a.c.k, next, k_slot, true);
 
-        // register i is the key at j0 + 4 half + 8 (i / 4) + i % 4
+        // register i is the key at j0 + 4 half + place(i)
+        auto place = [](int i) { return 8 * (i / 4) + i % 4; };
+        const float distance = (float)(r.at - j0 - 4 * half);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-            x[i] = __builtin_fmaf(-slope, fabsf((float)(r.at - j0 - 4 * half - 8 * (i / 4) - i % 4)), score_of<CAP>(x[i], rule));
+        for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(-slope, fabsf(distance - (float)place(i)), score_of<CAP>(x[i], rule));
         if (part) {
+            const uint32_t seen = seen_bits(j0, r.lo, r.hi, 4 * half);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int j = j0 + 4 * half + 8 * (i / 4) + i % 4;
-                x[i] = j >= r.lo && j < r.hi ? x[i] : kMinusInf;
-            }
+            for (int i = 0; i < 16; ++i) x[i] = if_seen(x[i], seen, place(i));
         }
         float best = x[0];
 #pragma unroll
