@@ -99,7 +99,7 @@ struct AppendArgs {
     const int32_t* lens;
     int64_t q_stride, kv_stride, q_out_stride;
     int n_pos, rot, axes, section0, section01, interleaved;  // section01: pairs of the first two axes
-    int heads, n_tokens;
+    int heads, n_tokens, waves_per_token;
 };
 int launch_rope_append(const AppendArgs& a, hipStream_t st);
 

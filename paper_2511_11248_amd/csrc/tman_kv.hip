@@ -7,12 +7,12 @@ namespace {
 
 // ---- rotary positions and append
 //
-// A wave takes one token and a run of its head rows (queries, then keys, then values).  A unit of work is 16 elements of a
+// A wave takes one token and some of its head rows (queries, then keys, then values).  A unit of work is 16 elements of a
 // head: eight pairs that turn, or 16 elements that are copied; D / 16 lanes make a head, so a wave takes 1024 / D heads at once
 // and the angles of a lane's pairs are the same for all heads and are read once.
 constexpr int kAppendWaves = 4;
+constexpr int kAppendRuns = 4096;  // waves that fill the chip
 
-template <class T>
 __device__ __forceinline__ void turn_pair(float& x, float& y, float c, float s) {
     const float a = x, b = y;
     x = __builtin_fmaf(a, c, -(b * s));
@@ -23,7 +23,8 @@ template <class T, int D>
 __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendArgs a) {
     constexpr int kUnits = D / 16, kRows = 64 / kUnits;  // head rows a wave takes at once
     const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
-    const int n = blockIdx.x;
+    const int run = (int)blockIdx.x * kAppendWaves + wave, n = run / a.waves_per_token;
+    if (n >= a.n_tokens) return;
     const int unit = lane % kUnits, sub = lane / kUnits;
     const int G = a.c.kv_heads, rows = a.heads + 2 * G;
 
@@ -74,8 +75,8 @@ __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendAr
     // where a lane's 16 elements are: two runs of eight
     const int e0 = turns && !a.interleaved ? pair : unit * 16, e1 = turns && !a.interleaved ? a.rot / 2 + pair : unit * 16 + 8;
 
-    const int step = kRows * kAppendWaves * gridDim.y;
-    for (int r0 = ((int)blockIdx.y * kAppendWaves + wave) * kRows; r0 < rows; r0 += step) {
+    const int step = kRows * a.waves_per_token;
+    for (int r0 = (run - n * a.waves_per_token) * kRows; r0 < rows; r0 += step) {
         const int r = r0 + sub;
         if (r >= rows) continue;
         const uint8_t* from;
@@ -104,10 +105,10 @@ __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendAr
             }
             if (a.interleaved) {
 #pragma unroll
-                for (int p = 0; p < 8; ++p) turn_pair<T>(f[2 * p], f[2 * p + 1], c[p], s[p]);
+                for (int p = 0; p < 8; ++p) turn_pair(f[2 * p], f[2 * p + 1], c[p], s[p]);
             } else {
 #pragma unroll
-                for (int p = 0; p < 8; ++p) turn_pair<T>(f[p], f[8 + p], c[p], s[p]);
+                for (int p = 0; p < 8; ++p) turn_pair(f[p], f[8 + p], c[p], s[p]);
             }
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -130,6 +131,10 @@ __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendAr
 // where it fits (CACHE positions).
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
+// Weights of a few powers of two fall into a few dozen of the first pass's bins, and lanes that add to one bin wait for each other:
+// four copies of the bins, by lane, beside each other.
+constexpr int kCopies = 4;
+constexpr int kMostCached = 28672;  // positions whose keys LDS holds beside the bins
 
 __device__ __forceinline__ uint32_t ordered(float w) {
     if (w != w) return 0xffffffffu;  // NaN: larger than all
@@ -150,7 +155,7 @@ __device__ __forceinline__ int sum_up_to(int x, int lane) {
 template <int CACHE>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t cache[CACHE ? CACHE : 4];
-    __shared__ int bins[kBins];
+    __shared__ __attribute__((aligned(16))) int bins[kBins * kCopies];
     __shared__ int wave_larger[kSelectWaves], wave_equal[kSelectWaves];
     __shared__ int found_digit, found_above, found_count;
     const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
@@ -207,17 +212,22 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     constexpr int kShift[3] = {21, 10, 0}, kWidth[3] = {11, 11, 10};
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-        for (int x = threadIdx.x; x < kBins; x += kSelectThreads) bins[x] = 0;
+        for (int x = threadIdx.x; x < kBins * kCopies; x += kSelectThreads) bins[x] = 0;
         __syncthreads();
         const uint32_t digits = (1u << kWidth[pass]) - 1;
         each((int)threadIdx.x * 4, kSelectThreads * 4, others, [&](int j, u32x4 u) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (j + r < others && (u[r] & mask) == prefix) atomicAdd(&bins[(u[r] >> kShift[pass]) & digits], 1);
+                if (j + r < others && (u[r] & mask) == prefix) atomicAdd(&bins[((u[r] >> kShift[pass]) & digits) * kCopies + (lane & (kCopies - 1))], 1);
         });
         __syncthreads();
         // counts from the highest digit down, two digits a thread: where do they reach `want`?
-        const int high = kBins - 1 - 2 * (int)threadIdx.x, c0 = bins[high], c1 = bins[high - 1];
+        const int high = kBins - 1 - 2 * (int)threadIdx.x;
+        auto count = [&](int bin) {
+            const i32x4 n = *reinterpret_cast<const i32x4*>(bins + bin * kCopies);
+            return n.x + n.y + n.z + n.w;
+        };
+        const int c0 = count(high), c1 = count(high - 1);
         int run = sum_up_to(c0 + c1, lane);
         if (lane == 63) wave_larger[wave] = run;
         __syncthreads();
@@ -338,12 +348,13 @@ void launch_move(const EvictArgs& a, hipStream_t st) {
 }
 
 template <class T>
-void launch_append(const AppendArgs& a, hipStream_t st) {
-    // a wave for at most 1024 / D head rows of a token where there are few tokens, all of a token's rows for four waves where
-    // they fill the chip
-    const int at_once = 1024 / a.c.dim * kAppendWaves, most = (a.heads + 2 * a.c.kv_heads + at_once - 1) / at_once;
-    const int parts = a.n_tokens >= 1024 ? 1 : most;
-    const dim3 grid(a.n_tokens, parts);
+void launch_append(AppendArgs a, hipStream_t st) {
+    // A wave for each 1024 / D head rows of a token where there are few tokens; finding a token's place takes longer than moving those, so
+    // where there are many a wave takes more of a token.
+    const int at_once = 1024 / a.c.dim, most = (a.heads + 2 * a.c.kv_heads + at_once - 1) / at_once;
+    a.waves_per_token = a.n_tokens >= kAppendRuns ? 1 : kAppendRuns / a.n_tokens;
+    if (a.waves_per_token > most) a.waves_per_token = most;
+    const int grid = (int)(((int64_t)a.n_tokens * a.waves_per_token + kAppendWaves - 1) / kAppendWaves);
     if (a.c.dim == 64) rope_append_kernel<T, 64><<<grid, kAppendWaves * 64, 0, st>>>(a);
     else if (a.c.dim == 128) rope_append_kernel<T, 128><<<grid, kAppendWaves * 64, 0, st>>>(a);
     else rope_append_kernel<T, 256><<<grid, kAppendWaves * 64, 0, st>>>(a);
@@ -361,7 +372,7 @@ int launch_kv_evict(const EvictArgs& a, hipStream_t st) {
     // what is weighed is kept in LDS where that holds it; the small form leaves room for two workgroups a unit
     const dim3 grid(a.c.kv_heads, a.c.n_seqs);
     if (a.max_len <= 8192) evict_select_kernel<8192><<<grid, kSelectThreads, 0, st>>>(a);
-    else if (a.max_len <= 32768) evict_select_kernel<32768><<<grid, kSelectThreads, 0, st>>>(a);
+    else if (a.max_len <= kMostCached) evict_select_kernel<kMostCached><<<grid, kSelectThreads, 0, st>>>(a);
     else evict_select_kernel<0><<<grid, kSelectThreads, 0, st>>>(a);
     if (a.c.dim == 64) launch_move<64>(a, st);
     else if (a.c.dim == 128) launch_move<128>(a, st);
