@@ -26,10 +26,12 @@ int check_cache(const tman_kv_cache_t* c) {
     return aligned16(c->k_pages) && aligned16(c->v_pages) ? TMAN_OK : TMAN_ERR_ALIGN;
 }
 
-// heads <= 16 * kGridMost / kv_heads keeps a decode launch's grid in range
 int check_heads(const tman_kv_cache_t* c, int32_t heads) {
     return heads >= 1 && heads <= 65536 && heads % c->kv_heads == 0 ? TMAN_OK : TMAN_ERR_SHAPE;
 }
+
+// rows of queries are numbered in 32 bits
+bool too_many_rows(int64_t tokens, int32_t heads) { return tokens * heads > 0x7fffffff; }
 
 int check_attn(const tman_kv_cache_t* c, const tman_attn_t* a, int32_t max_len) {
     if (!a) return TMAN_ERR_NULL;
@@ -73,7 +75,7 @@ int tman_rope_append(const tman_kv_cache_t* cache, const tman_rope_t* rope, int3
                      void* stream) {
     int rc = check_cache(cache);
     if (rc != TMAN_OK) return rc;
-    if (n_tokens < 1 || (!q_start && n_tokens != cache->n_seqs)) return TMAN_ERR_SHAPE;
+    if (n_tokens < 1 || n_tokens > kMostPositions || (!q_start && n_tokens != cache->n_seqs)) return TMAN_ERR_SHAPE;
     if (!lens || (q == nullptr) != (q_out == nullptr)) return TMAN_ERR_NULL;
     if (q) {
         if (check_heads(cache, heads) != TMAN_OK) return TMAN_ERR_SHAPE;
@@ -123,7 +125,7 @@ int tman_rope_append(const tman_kv_cache_t* cache, const tman_rope_t* rope, int3
 }
 
 size_t tman_attn_decode_workspace_bytes(const tman_kv_cache_t* cache, const tman_attn_t* attn, int32_t max_len, int32_t weights) {
-    if (check_cache_sizes(cache) != TMAN_OK || check_attn(cache, attn, max_len) != TMAN_OK) return 0;
+    if (check_cache_sizes(cache) != TMAN_OK || check_attn(cache, attn, max_len) != TMAN_OK || too_many_rows(cache->n_seqs, attn->heads)) return 0;
     return plan_attn_decode(cache, attn, max_len, weights != 0).bytes;
 }
 
@@ -133,6 +135,7 @@ int tman_attn_decode(const tman_kv_cache_t* cache, const tman_attn_t* attn, cons
     int rc = check_cache(cache);
     if (rc != TMAN_OK) return rc;
     if ((rc = check_attn(cache, attn, max_len)) != TMAN_OK) return rc;
+    if (too_many_rows(cache->n_seqs, attn->heads)) return TMAN_ERR_SHAPE;
     if (!lens) return TMAN_ERR_NULL;
     if ((rc = check_rows(q, q_stride, attn->heads, cache->dim)) != TMAN_OK) return rc;
     if ((rc = check_rows(out, out_stride, attn->heads, cache->dim)) != TMAN_OK) return rc;
@@ -167,7 +170,7 @@ int tman_attn_decode(const tman_kv_cache_t* cache, const tman_attn_t* attn, cons
 
 size_t tman_attn_prefill_workspace_bytes(const tman_kv_cache_t* cache, const tman_attn_t* attn, int32_t n_tokens, int32_t max_len) {
     if (check_cache_sizes(cache) != TMAN_OK || check_attn(cache, attn, max_len) != TMAN_OK || n_tokens < 1) return 0;
-    if ((int64_t)n_tokens * attn->heads > 0x7fffffff) return 0;
+    if (too_many_rows(n_tokens, attn->heads)) return 0;
     return plan_attn_prefill(cache, attn, n_tokens, max_len).bytes;
 }
 
@@ -177,7 +180,7 @@ int tman_attn_prefill(const tman_kv_cache_t* cache, const tman_attn_t* attn, int
     int rc = check_cache(cache);
     if (rc != TMAN_OK) return rc;
     if ((rc = check_attn(cache, attn, max_len)) != TMAN_OK) return rc;
-    if (n_tokens < 1 || (int64_t)n_tokens * attn->heads > 0x7fffffff) return TMAN_ERR_SHAPE;
+    if (n_tokens < 1 || too_many_rows(n_tokens, attn->heads)) return TMAN_ERR_SHAPE;
     if (!lens || !q_start) return TMAN_ERR_NULL;
     if ((rc = check_rows(q, q_stride, attn->heads, cache->dim)) != TMAN_OK) return rc;
     if ((rc = check_rows(out, out_stride, attn->heads, cache->dim)) != TMAN_OK) return rc;

@@ -193,5 +193,12 @@ def test_binding_refuses_tensors_that_do_not_fit():
     assert status(lambda: evict(new_table=torch.zeros(3, 1, dtype=torch.int32))) == SHAPE
 
 
+def test_rows_are_numbered_in_32_bits():
+    L, c, a = at._load(), _cache(n_seqs=65535, kv_heads=2), _attn(heads=65536)
+    assert _decode(L, c, a, qs=1 << 23, os=1 << 23) == SHAPE and L.tman_attn_decode_workspace_bytes(c, a, 64, 0) == 0
+    assert _prefill(L, c, a, n=40000, qs=1 << 23, os=1 << 23) == SHAPE and L.tman_attn_prefill_workspace_bytes(c, a, 40000, 64) == 0
+    assert _append(L, c, n=(1 << 30) + 1, start=FAKE) == SHAPE
+
+
 def test_status_strings():
     assert len({tman.tman_status_string(c) for c in range(0, -11, -1)}) == 11
