@@ -60,7 +60,6 @@ struct PrefillPlan {
     int row_tiles;  // at most, over all sequences
     int n_split;    // pieces, at most
     int n_slots;    // of partial sums for an item (few)
-    int fold;       // the first so many workgroups of a key-value head take the last row tiles, from the last; the others from the first
     size_t partial_at, count_at, bytes;
 };
 PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len);

@@ -1,16 +1,23 @@
 // Attention of the new tokens of prompts over a paged cache.
 //
-// What bounds it: the matrix cores, and beside them the vector pipe, which makes an exponential and about six other operations of
-// every score that the matrix cores spend 4 * dim operations on.
+// What bounds it: the power the chip may take, the matrix cores and beside them the vector pipe, which makes an exponential (two issue
+// slots) and four other operations of every score that the matrix cores spend 4 * dim operations on (capped: two exponentials, a reciprocal
+// and six).  8192 tokens, 32 heads of 128 over 8, causal: 546 us = 1.0 PFLOP/s with the matrix cores busy 55 % of the cycles at 1.8 GHz
+// (the library's plain product of 8192^3: 1.16); capped 626 us; heads of 64 0.82, of 256 0.84 PFLOP/s.
 //   * A workgroup takes 128 rows of one sequence and one key-value head - new tokens times the query heads of the group, so that
 //     the heads that share keys share the tiles of them - and walks over tiles of 64 positions, of which it sees an interval.
-//   * Keys and values of the next tile go straight into LDS while the present one is worked on (two buffers).
+//   * Keys and values of the tiles ahead go straight into LDS while the present one is worked on, one barrier a tile.
+//   * The products of the next tile's keys are made between the exponentials of the present one, in an order of issue that is set
+//     (the wave's own vector work hides beside its products; 4 %, heads of 256 12 %).
 //   * Scores are K q^T with a key a row and a query a column (32x32x16): a lane holds 32 scores of ONE query, so the softmax needs
 //     one exchange between two half waves, and the probabilities are, as they are, the operand of out^T = V^T P^T; V^T is
 //     read from LDS by columns in the same order of keys.
 //   * Only tiles in which some query of a wave does not see all keys compare positions.  There a hidden value may be anything,
 //     infinity and NaN included: such tiles are looked through, and what is not finite is left out of the products and added
 //     where it is seen.
+// Measured and not better: 8 waves and 256 rows a workgroup (equal), tiles in a rising and a falling order (equal), issue priorities
+// (5 % slower), three workgroups a unit for heads of 64 (equal; 6 % slower on long caches).  Without the requests for keys and
+// values the loop takes 9 % less.
 #include <type_traits>
 
 #include "tman_attn_join.h"
@@ -21,16 +28,14 @@ namespace {
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kMaxSplit = 64;
 static_assert(kManyRows == kWaves * 32, "a wave takes 32 rows");
+// How far the largest score may run ahead of the reference of the exponentials, in powers of two.
 constexpr float kSlack = 8.f;
+constexpr int kLeastTiles = 8;  // of 64 positions, of a piece
+// The order of issue in the loop over whole tiles: how many reads of LDS run ahead of the products of keys and of values, and how many
+// operations of the vector pipe go beside each of these products.  (4 to 10 and 4 to 12 reads, 3 to 6 operations: within 1 %; without
+// an order 4 % slower.)
+constexpr int kKeysAhead = 6, kValuesAhead = 8, kBesideKeys = 4, kBesideValues = 3;
 constexpr int kVector = 0x2, kMatrix = 0x8, kReadsLds = 0x100;  // kinds of instructions, for the scheduler
-#ifndef BESIDE
-#define BESIDE 4
-#define BESIDE2 3
-#define AHEAD2 8
-#define AHEAD 6
-#endif
-constexpr int kBeside = BESIDE, kBeside2 = BESIDE2;
-constexpr int kLeastTiles = 8;  // of a piece
 
 // Positions of a tile: heads of 256 leave registers for the scores of 32.
 __host__ __device__ constexpr int tile_of(int D) { return D == 256 ? 32 : 64; }
@@ -41,9 +46,6 @@ __host__ __device__ constexpr int buffers_of(int D) { return D == 128 ? 2 : 4; }
 
 // [item][piece]: every wave's accumulators as they lie in its lanes, then the maxima and sums of its columns
 __host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kManyRows * D + 2 * kManyRows; }
-
-// the row tile of workgroup number r of a key-value head (and piece)
-__device__ __forceinline__ int item_of(const PrefillPlan& p, int r) { return r < p.fold ? p.row_tiles - 1 - r : r - p.fold; }
 
 // 32 coordinates of a row: register 4 i + x of a lane is coordinate 8 i + 4 half + x
 template <class T>
@@ -74,7 +76,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
 
     // which rows: the heaviest (the last) first, key-value heads over the XCDs
     const int hk = (int)blockIdx.x % a.c.kv_heads, rest = (int)blockIdx.x / a.c.kv_heads;
-    const int piece = rest % a.p.n_split, item = item_of(a.p, rest / a.p.n_split);
+    const int piece = rest % a.p.n_split, item = a.p.row_tiles - 1 - rest / a.p.n_split;
     const RowTile rows = find_row_tile<kManyRows>(a, item, lane);
     if (rows.b < 0) {
         if (a.p.n_split > 1 && piece == 0 && threadIdx.x == 0) a.counts[(int64_t)item * a.c.kv_heads + hk] = 0;
@@ -273,20 +275,20 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             if constexpr (!PART) {
                 // The order of issue: reads of LDS run ahead of the products that take them, and the vector pipe has something to do
                 // beside every product.
-                constexpr int kAhead = AHEAD, kQk = kKeyBlocks * (D / 16), kPv = 2 * kKeyBlocks * kBlocks;
-                __builtin_amdgcn_sched_group_barrier(kReadsLds, kAhead, 0);
+                constexpr int kQk = kKeyBlocks * (D / 16), kPv = 2 * kKeyBlocks * kBlocks;
+                __builtin_amdgcn_sched_group_barrier(kReadsLds, kKeysAhead, 0);
 #pragma unroll
                 for (int x = 0; x < kQk; ++x) {
                     __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(kReadsLds, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kVector, kBeside, 0);
+                    __builtin_amdgcn_sched_group_barrier(kVector, kBesideKeys, 0);
                 }
-                __builtin_amdgcn_sched_group_barrier(kReadsLds, AHEAD2, 0);
+                __builtin_amdgcn_sched_group_barrier(kReadsLds, kValuesAhead, 0);
 #pragma unroll
                 for (int x = 0; x < kPv; ++x) {
                     __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(kReadsLds, 2, 0);
-                    __builtin_amdgcn_sched_group_barrier(kVector, kBeside2, 0);
+                    __builtin_amdgcn_sched_group_barrier(kVector, kBesideValues, 0);
                 }
             }
         } else {
@@ -493,10 +495,6 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     p.n_split = (int)pieces;
     p.n_slots = piece_slots(p.n_split);
     p.second = pieces > 1 && (!p.few || rows > kFewJoined * seqs);
-    // Two workgroups fit a unit.  Where all are there at once, the second half goes the other way, so that a unit has a long and a short
-    // one (causal rows); where there are more, a unit takes the next as one ends, and the longest go first.
-    const int64_t grid = items * pieces, half = ceil_div(kUnits, c->kv_heads * pieces);
-    p.fold = (int)(!p.few && grid > kUnits && grid <= 2 * kUnits && half < tiles ? half : tiles);
     p.partial_at = kAttnTicketBytes;
     if (pieces > 1) {
         p.count_at = p.partial_at + items * (p.few ? p.n_slots * ((size_t)kFewRows * c->dim + 2 * kFewRows) : pieces * partial_floats(c->dim)) * sizeof(float);

@@ -4,6 +4,8 @@
 // tokens times the query heads of the group - and one piece of the positions; its waves take tiles of 32 positions in turn,
 // each through slots of its own in LDS, and meet at the end; pieces meet in the workspace.  Scores are K q^T with a key a row and a query a
 // column (32x32x16), so that the probabilities are the operand of out^T = V^T P^T as they are.
+// 32 heads of 128 over 8, one token at 16384: 19 us (3.6 TB/s), 8 tokens 23, 64 tokens of their own 7 us.  The last workgroup to arrive
+// adds up to 8 rows a sequence; more go to a second kernel (4 tokens at 4096 17 and 21 us, 8 tokens at 16384 35 and 23).
 #include "tman_attn_join.h"
 
 namespace tman {

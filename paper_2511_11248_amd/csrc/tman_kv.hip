@@ -10,6 +10,9 @@ namespace {
 // A wave takes one token and some of its head rows (queries, then keys, then values).  A unit of work is 16 elements of a
 // head: eight pairs that turn, or 16 elements that are copied; D / 16 lanes make a head, so a wave takes 1024 / D heads at once
 // and the angles of a lane's pairs are the same for all heads and are read once.
+// 5461 tokens of 3 x 32 heads: 62 us (271 MB, 4.35 TB/s; a large copy reaches 5.1), 4096 tokens of 32 heads over 8: 22 us.  Reading the next rows
+// ahead of writing the present ones is no faster (66 us); a wave that takes a sixth of a token only is slower (25.5 us), since
+// finding the token's place is a chain of reads.
 constexpr int kAppendWaves = 4;
 constexpr int kAppendRuns = 4096;  // waves that fill the chip
 
@@ -127,7 +130,7 @@ __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendAr
 // integer form, up to three passes of 11, 11 and 10 bits, each of which counts the digits of what is still undecided and keeps the
 // digit in which the last chosen one lies; it ends early where all with that digit are chosen.  What then equals the threshold
 // goes to the lowest positions.
-// What bounds it: one unit's latency, so everything is read four positions at a time with several reads under way, and kept in LDS
+// 16384 positions of 128 heads: 18 us, 2049 of 32 heads 7.  What bounds it: one unit's latency, so everything is read four positions at a time with several reads under way, and kept in LDS
 // where it fits (CACHE positions).
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
@@ -297,6 +300,8 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 }
 
 // ---- eviction: the kept rows move
+//
+// Whole rows, four a thread under way: 16 x 8 heads x 4096 rows 108 us (4.6 TB/s of the 5.1 that a large copy reaches).
 constexpr int kMoveThreads = 256;
 
 template <int D>
