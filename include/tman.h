@@ -4,7 +4,8 @@
  * The library implements the hot path of T-MAN (arxiv 2511.11248): the product of group-quantized
  * 1/2/4-bit weights with fp16 activations, y = x * dequant(W)^T, computed through table lookup --
  * bit-serial activation tables for decoding (mpGEMV) and a two-level table dequantization feeding
- * the matrix cores for prefill (mpGEMM) -- from ONE bit-serial packed copy of the weights.
+ * the matrix cores for prefill (mpGEMM) -- from ONE bit-serial packed copy of the weights.  Next to it stand the operators
+ * between a layer's products: a key-value cache in pages, attention over it, eviction (see "Key-value cache in pages").
  *
  * Conventions for every call
  *   - all data pointers are DEVICE pointers unless stated otherwise; the caller owns every buffer,
@@ -514,7 +515,8 @@ int tman_attn_decode(const tman_kv_cache_t *cache, const tman_attn_t *attn, cons
  *   packed documents  first[n] = the start of n's document
  *   a prefix          end[n] = max(i + 1, length of the prefix): seen by all, also by the tokens inside
  * or any other interval.  A token that sees nothing gives zeros, and minus infinity in lse (fp32 [n_tokens][heads] or NULL).
- * Hidden keys and values never reach a result, whatever they hold (infinities and NaN too).
+ * Hidden keys and values never reach a result, whatever they hold (infinities and NaN too); an infinite value that is seen makes
+ * the result infinite or NaN.
  *   workspace : at least tman_attn_prefill_workspace_bytes for the same cache, attn and n_tokens and for max_len or more (0:
  *               NULL will do); as for tman_attn_decode
  *   max_len   : no sequence is longer

@@ -47,14 +47,19 @@ __host__ __device__ constexpr int buffers_of(int D) { return D == 128 ? 2 : 4; }
 // [item][piece]: every wave's accumulators as they lie in its lanes, then the maxima and sums of its columns
 __host__ __device__ constexpr size_t partial_floats(int D) { return (size_t)kManyRows * D + 2 * kManyRows; }
 
-// 32 coordinates of a row: register 4 i + x of a lane is coordinate 8 i + 4 half + x
+// 32 coordinates of a row: register 4 i + x of a lane is coordinate 8 i + 4 half + x.  The halves of a row's lanes exchange every second four,
+// so that each stores 16 bytes at once.
 template <class T>
 __device__ __forceinline__ void store_block(uint8_t* to, const f32x16& out, float inv, bool empty, int half) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        u32x2 w = {T::pack(out[4 * i] * inv, out[4 * i + 1] * inv), T::pack(out[4 * i + 2] * inv, out[4 * i + 3] * inv)};
-        if (empty) w = u32x2{0, 0};  // nothing seen, or nothing of any weight
-        *reinterpret_cast<u32x2*>(to + (8 * i + 4 * half) * 2) = w;
+    for (int i = 0; i < 4; i += 2) {
+        const auto x = __builtin_amdgcn_permlane32_swap(T::pack(out[4 * i] * inv, out[4 * i + 1] * inv),
+                                                        T::pack(out[4 * i + 4] * inv, out[4 * i + 5] * inv), false, false);
+        const auto y = __builtin_amdgcn_permlane32_swap(T::pack(out[4 * i + 2] * inv, out[4 * i + 3] * inv),
+                                                        T::pack(out[4 * i + 6] * inv, out[4 * i + 7] * inv), false, false);
+        u32x4 w = {x[0], y[0], x[1], y[1]};
+        if (empty) w = u32x4{0, 0, 0, 0};  // nothing seen, or nothing of any weight
+        *reinterpret_cast<u32x4*>(to + (8 * i + 8 * half) * 2) = w;
     }
 }
 
