@@ -97,17 +97,13 @@ class KvCache:
 
     def _rows(self, t, where: str, heads: int, tokens: int) -> int:
         """Stride between tokens of t [tokens][heads][dim], whose heads must be contiguous."""
-        if t is None:
-            raise TmanError(_ERR_NULL, where)
-        shape, strides = t.shape, t.stride()
-        if len(shape) != 3 or shape[0] != tokens or shape[1] != heads or shape[2] != self.dim:
+        dim = self.dim
+        if t is None or t.shape != (tokens, heads, dim) or t.dtype is not self.dtype:
+            raise TmanError(_ERR_NULL if t is None else _ERR_SHAPE if t.shape != (tokens, heads, dim) else _ERR_CACHE, where)
+        stride, head, element = t.stride()
+        if element != 1 or (head != dim and heads != 1):
             raise TmanError(_ERR_SHAPE, where)
-        if t.dtype is not self.dtype:
-            raise TmanError(_ERR_CACHE, where)
-        stride, head, element = strides
-        if element != 1 or (head != self.dim and heads != 1):
-            raise TmanError(_ERR_SHAPE, where)
-        return stride if tokens > 1 else max(stride, heads * self.dim)
+        return stride if tokens > 1 else max(stride, heads * dim)
 
     def _weights(self, t, where: str) -> int:
         _wants(t.shape == self.k_pages.shape[:3] and _is(t, _float32), where)
@@ -157,12 +153,9 @@ def _floats(t, n: int, where: str) -> int:
     return t.data_ptr()
 
 
-def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None, weights=None,
-                     stream=None) -> None:
-    """Rotates q and k (q_out may be q; both None: no queries) and writes k and v [n_tokens][kv_heads][dim] into the cache as the
-    last positions of their sequences; q_start None: one token a sequence."""
-    where = "tman_rope_append"
-    _wants(k is not None, where, _ERR_NULL)
+def _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights):
+    if k is None:
+        raise TmanError(_ERR_NULL, where)
     n, B = k.shape[0], cache.n_seqs
     kv_stride = cache._rows(k, where, cache.kv_heads, n)
     if cache._rows(v, where, cache.kv_heads, n) != kv_stride:
@@ -171,32 +164,64 @@ def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, po
     if q is not None:
         heads = q.shape[1]
         q_stride, q_out_stride = cache._rows(q, where, heads, n), cache._rows(q_out, where, heads, n)
-    _wants(positions is None or rope is not None, where)
+    if positions is not None and rope is None:
+        raise TmanError(_ERR_SHAPE, where)
+    return (cache._ref, None if rope is None else rope._ref, heads, n, None if q is None else q.data_ptr(), q_stride, k.data_ptr(),
+            v.data_ptr(), kv_stride, None if positions is None else _ints(positions, len(rope.sections) * n, where),
+            None if q_start is None else _ints(q_start, B + 1, where), _ints(lens, B, where),
+            None if q_out is None else q_out.data_ptr(), q_out_stride, None if weights is None else cache._weights(weights, where))
+
+
+def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None, weights=None,
+                     stream=None) -> None:
+    """Rotates q and k (q_out may be q; both None: no queries) and writes k and v [n_tokens][kv_heads][dim] into the cache as the
+    last positions of their sequences; q_start None: one token a sequence."""
+    where = "tman_rope_append"
     L = _functions or _load()
-    _check(L.tman_rope_append(cache._ref, None if rope is None else rope._ref, heads, n, None if q is None else q.data_ptr(), q_stride,
-                              k.data_ptr(), v.data_ptr(), kv_stride,
-                              None if positions is None else _ints(positions, len(rope.sections) * n, where),
-                              None if q_start is None else _ints(q_start, B + 1, where), _ints(lens, B, where),
-                              None if q_out is None else q_out.data_ptr(), q_out_stride,
-                              None if weights is None else cache._weights(weights, where), _stream(stream)), where)
+    _check(L.tman_rope_append(*_append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights), _stream(stream)), where)
+
+
+def bound_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None, weights=None):
+    """The same, checked and marshalled once for calls that run every step with the same tensors: call(stream_handle)."""
+    where = "tman_rope_append"
+    fn, args = _load().tman_rope_append, _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights)
+
+    def call(stream_handle):
+        _check(fn(*args, stream_handle), where)
+
+    return call
 
 
 def tman_attn_decode_workspace_bytes(cache: KvCache, attn: Attn, max_len: int, weights: bool = False) -> int:
     return int(_load().tman_attn_decode_workspace_bytes(cache._ref, attn._ref, max_len, 1 if weights else 0))
 
 
+def _decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights):
+    B, H = cache.n_seqs, attn.heads
+    return (cache._ref, attn._ref, None if q is None else q.data_ptr(), cache._rows(q, where, H, B), _ints(lens, B, where),
+            None if first is None else _ints(first, B, where), max_len, None if out is None else out.data_ptr(),
+            cache._rows(out, where, H, B), None if lse is None else _floats(lse, B * H, where),
+            None if weights is None else cache._weights(weights, where), None if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.nbytes)
+
+
 def tman_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, workspace, first=None, lse=None, weights=None,
                      stream=None) -> None:
     """Attention of one new token of every sequence over its cache; the workspace is zero-filled once by the caller."""
     where = "tman_attn_decode"
-    B, H = cache.n_seqs, attn.heads
     L = _functions or _load()
-    _check(L.tman_attn_decode(cache._ref, attn._ref, None if q is None else q.data_ptr(), cache._rows(q, where, H, B), _ints(lens, B, where),
-                              None if first is None else _ints(first, B, where), max_len, None if out is None else out.data_ptr(),
-                              cache._rows(out, where, H, B), None if lse is None else _floats(lse, B * H, where),
-                              None if weights is None else cache._weights(weights, where),
-                              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
-                              _stream(stream)), where)
+    _check(L.tman_attn_decode(*_decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights), _stream(stream)), where)
+
+
+def bound_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, workspace, first=None, lse=None, weights=None):
+    """The same, checked and marshalled once; max_len bounds the lengths of all the steps: call(stream_handle)."""
+    where = "tman_attn_decode"
+    fn, args = _load().tman_attn_decode, _decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights)
+
+    def call(stream_handle):
+        _check(fn(*args, stream_handle), where)
+
+    return call
 
 
 def tman_attn_prefill_workspace_bytes(cache: KvCache, attn: Attn, n_tokens: int, max_len: int) -> int:

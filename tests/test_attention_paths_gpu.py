@@ -123,3 +123,34 @@ def test_append_prompt_and_eviction_in_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(state(), want))
     assert tman.tman_device_status() == 0
+
+
+def test_bound_calls_do_what_the_calls_do():
+    """Checked once, run every step: the same bits as the calls, on the stream that they are given, refusals at once."""
+    H, G, D, B = 6, 2, 128, 3
+    P = Problem(55, [40, 700, 9], H, G, D, 32, torch.float16, poison=0.0)
+    attn = tman.Attn(H, 0.09)
+    qkv, out, want = P.normal(B, H + 2 * G, D), *(torch.empty(B, H, D, dtype=P.dtype, device=dev()) for _ in range(2))
+    q, k, v, turned = qkv[:, :H], qkv[:, H:H + G], qkv[:, H + G:], torch.empty(B, H, D, dtype=P.dtype, device=dev())
+    angle = torch.rand(1000, D // 2, generator=P.gen, device=dev()) * 6
+    rope = tman.Rope(torch.stack([angle.cos(), angle.sin()], -1).contiguous())
+    ws = torch.zeros(tman.tman_attn_decode_workspace_bytes(P.cache, attn, 800), dtype=torch.uint8, device=dev())
+    append = tman.bound_rope_append(P.cache, q, k, v, P.lens, turned, rope=rope)
+    decode = tman.bound_attn_decode(P.cache, attn, turned, P.lens, out, 800, ws)
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        P.lens -= 1
+        qkv.copy_(P.normal(*qkv.shape))
+        torch.cuda.synchronize()
+        append(s.cuda_stream)
+        decode(s.cuda_stream)
+        s.synchronize()
+        pages, queries = P.k.clone(), turned.clone()
+        tman.tman_rope_append(P.cache, q, k, v, P.lens, turned, rope=rope)
+        tman.tman_attn_decode(P.cache, attn, turned, P.lens, want, 800, ws)
+        assert torch.equal(out, want) and torch.equal(P.k, pages) and torch.equal(turned, queries)
+    assert tman.tman_device_status() == 0
+    with pytest.raises(tman.TmanError):
+        tman.bound_attn_decode(P.cache, attn, turned[:2], P.lens, out, 800, ws)
+    with pytest.raises(tman.TmanError):
+        tman.bound_rope_append(P.cache, q, k, v, P.lens, None, rope=rope)
