@@ -175,6 +175,20 @@ struct RowsOf {
     static constexpr __host__ __device__ uint32_t value_turn32(uint32_t r) { return (D == 64 ? (r >> 1) & 1 : r & 3) << 2; }
 };
 
+// Sum of x over the lanes up to this one: within rows of 16 lanes, then a row's last lane to the rows behind it.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int plus_shifted(int x) {
+    return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int sum_up_to(int x) {
+    x = plus_shifted<0x111, 0xf>(x);  // from one lane below,
+    x = plus_shifted<0x112, 0xf>(x);  // two,
+    x = plus_shifted<0x114, 0xf>(x);  // four,
+    x = plus_shifted<0x118, 0xf>(x);  // eight,
+    x = plus_shifted<0x142, 0xa>(x);  // the last lane of rows 0 and 2 to rows 1 and 3,
+    return plus_shifted<0x143, 0xc>(x);  // lane 31 to rows 2 and 3
+}
+
 // Rows of a prompt's launch: the new tokens of a sequence times the query heads of a key-value head, in tiles of ROWS rows, all
 // sequences' tiles one after another.
 struct RowTile {
@@ -196,14 +210,7 @@ __device__ __forceinline__ RowTile find_row_tile(const PrefillArgs& a, int item,
             n = min(max(n, s0), a.n_tokens) - s0;
         }
         const int tiles = (int)(((int64_t)n * a.group + ROWS - 1) / ROWS);
-        int run = tiles;
-        if (a.c.n_seqs > 1) {
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int other = __shfl_up(run, d);
-                if (lane >= d) run += other;
-            }
-        }
+        const int run = sum_up_to(tiles);
         const uint64_t found = __ballot(run > r.tile);
         if (found) {
             const int l = __builtin_ctzll(found);

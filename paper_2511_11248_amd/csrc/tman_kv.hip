@@ -145,16 +145,6 @@ __device__ __forceinline__ uint32_t ordered(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Inclusive sum over the lanes up to this one.
-__device__ __forceinline__ int sum_up_to(int x, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int other = __shfl_up(x, d);
-        if (lane >= d) x += other;
-    }
-    return x;
-}
-
 template <int CACHE>
 __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs a) {
     __shared__ __attribute__((aligned(16))) uint32_t cache[CACHE ? CACHE : 4];
@@ -231,7 +221,7 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
             return n.x + n.y + n.z + n.w;
         };
         const int c0 = count(high), c1 = count(high - 1);
-        int run = sum_up_to(c0 + c1, lane);
+        int run = sum_up_to(c0 + c1);
         if (lane == 63) wave_larger[wave] = run;
         __syncthreads();
         for (int w = 0; w < wave; ++w) run += wave_larger[w];
