@@ -1,5 +1,7 @@
 // What writes a paged cache (rotary positions and the append of new tokens) and what makes room in it (eviction by
-// accumulated attention weight).  All of it is bound by HBM: every element is read once and written once.
+// accumulated attention weight).  All of it is bound by HBM: every element is read once and written once.  The rows are stored
+// as a stream that second-level caches need not keep: 5461 tokens of 3 x 32 heads 63 -> 60 us, 4096 of 32 over 8 22.5 -> 19.5; the
+// attention that reads a few appended rows next takes as long as before (append and decode of 500 positions 9.6 and 9.9 us).
 #include "tman_attn_device.h"
 
 namespace tman {
@@ -10,7 +12,7 @@ namespace {
 // A wave takes one token and some of its head rows (queries, then keys, then values).  A unit of work is 16 elements of a
 // head: eight pairs that turn, or 16 elements that are copied; D / 16 lanes make a head, so a wave takes 1024 / D heads at once
 // and the angles of a lane's pairs are the same for all heads and are read once.
-// 5461 tokens of 3 x 32 heads: 62 us (271 MB, 4.35 TB/s; a large copy reaches 5.1), 4096 tokens of 32 heads over 8: 22 us.  Reading the next rows
+// 5461 tokens of 3 x 32 heads: 60 us (271 MB, 4.5 TB/s; a large copy reaches 5.1), 4096 tokens of 32 heads over 8: 19.5 us.  Reading the next rows
 // ahead of writing the present ones is no faster (66 us); a wave that takes a sixth of a token only is slower (25.5 us), since
 // finding the token's place is a chain of reads.
 constexpr int kAppendWaves = 4;
@@ -119,8 +121,8 @@ __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendAr
                 y[w] = T::pack(f[8 + 2 * w], f[8 + 2 * w + 1]);
             }
         }
-        *reinterpret_cast<u32x4*>(to + e0 * 2) = x;
-        *reinterpret_cast<u32x4*>(to + e1 * 2) = y;
+        __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to + e0 * 2));
+        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(to + e1 * 2));
     }
 }
 
@@ -291,12 +293,13 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
 
 // ---- eviction: the kept rows move
 //
-// Whole rows, four a thread under way: 16 x 8 heads x 4096 rows 108 us (4.6 TB/s of the 5.1 that a large copy reaches).
-constexpr int kMoveThreads = 256;
+// Whole rows, two a thread under way: 16 x 8 heads x 4096 rows 96 us (5.1 TB/s, as a large copy).  With the choice of
+// the rows 114 us; with four a thread 120, with four and ordinary stores 125.
+constexpr int kMoveThreads = 256, kRowsEach = 2;
 
 template <int D>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
-    constexpr int kLanes = D / 8, kRows = kMoveThreads / kLanes, kEach = 4;  // lanes a row, rows at once, rows a thread
+    constexpr int kLanes = D / 8, kRows = kMoveThreads / kLanes, kEach = kRowsEach;  // lanes a row, rows at once, rows a thread
     const int hk = blockIdx.y, b = blockIdx.z;
     const int n = min(checked_length(a.c, a.lens, b, a.max_len), a.keep);
     const int32_t* kept = a.kept + ((int64_t)b * a.c.kv_heads + hk) * a.keep;
@@ -330,15 +333,15 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
 #pragma unroll
     for (int x = 0; x < kEach; ++x) {
         if (to[x] < 0) continue;
-        reinterpret_cast<u32x4*>(a.c.k)[to[x] * kLanes + part] = k[x];
-        reinterpret_cast<u32x4*>(a.c.v)[to[x] * kLanes + part] = v[x];
+        __builtin_nontemporal_store(k[x], reinterpret_cast<u32x4*>(a.c.k) + to[x] * kLanes + part);
+        __builtin_nontemporal_store(v[x], reinterpret_cast<u32x4*>(a.c.v) + to[x] * kLanes + part);
         if (part == 0) a.weights[to[x]] = w[x];
     }
 }
 
 template <int D>
 void launch_move(const EvictArgs& a, hipStream_t st) {
-    const int rows = kMoveThreads / (D / 8) * 4;
+    const int rows = kMoveThreads / (D / 8) * kRowsEach;
     evict_move_kernel<D><<<dim3((a.keep + rows - 1) / rows, a.c.kv_heads, a.c.n_seqs), kMoveThreads, 0, st>>>(a);
 }
 
