@@ -128,6 +128,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
         wait_lds();  // the keys have been read
         if (more) request(a.c.k, next, k_slot, true);
 
+        if constexpr (CAP) {
+            auto capped = [&](auto score) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[u][r] = score(s[u][r], rule);
+            };
+            if (len - lo < kFewSeen) capped(score_of<CAP>);
+            else capped(score_in_many<CAP>);
+        }
         const bool part = j0 < lo || j0 + kTile > len;
         float best = kLowest;
 #pragma unroll
@@ -135,7 +145,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int j = j0 + 16 * u + 4 * g + r;
-                float x = __builtin_fmaf(-slope, (float)(at - j), score_of<CAP>(s[u][r], rule));
+                float x = __builtin_fmaf(-slope, (float)(at - j), CAP ? s[u][r] : score_of<CAP>(s[u][r], rule));
                 if (part) x = j >= lo && j < len ? x : kMinusInf;
                 s[u][r] = x;
                 best = fmaxf(best, x);

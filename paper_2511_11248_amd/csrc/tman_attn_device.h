@@ -146,14 +146,27 @@ struct ScoreRule {
         : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e) {}
 };
 // cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of 2^-23 cap, whatever x.  (exp2 and the reciprocal take the time of two
-// products each here, so a polynomial for small x is no faster: six products more in their place gave the same times.)
+// products each here, so a polynomial for small x is no faster: six products more in their place gave the same times.)  Right for
+// rows that see many positions; the kernel for many rows, which has no registers left, makes all scores so.
 template <bool CAP>
-__device__ __forceinline__ float score_of(float raw, const ScoreRule& r) {
+__device__ __forceinline__ float score_in_many(float raw, const ScoreRule& r) {
     if constexpr (!CAP) return raw * r.scale;
     const float e = __builtin_amdgcn_exp2f(raw * r.scale);
     return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap);
 }
-// the same less `top`, in one operation less
+// The same with a relative error of 2^-20: a row that sees a single position has its score as the logarithm of its sum.  Where a wave
+// has no row of fewer than kFewSeen positions, that error is spread over as many scores and not worth nine operations each.  Below
+// |x| = 1/2, cap tanh(x) = cap x (1 + z p(z)), z = (2x log2 e)^2, with p fitted to tanh here to 2^-26.
+constexpr int kFewSeen = 16;
+template <bool CAP>
+__device__ __forceinline__ float score_of(float raw, const ScoreRule& r) {
+    const float far = score_in_many<CAP>(raw, r);
+    if constexpr (!CAP) return far;
+    const float t = raw * r.scale, z = t * t, line = t * (r.cap * (0.5f / kLog2e));
+    const float p = __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(3.59193746e-6f, z, -9.19353042e-5f), z, 1.92256598e-3f), z, -4.00375277e-2f);
+    return z < kLog2e * kLog2e ? __builtin_fmaf(line, z * p, line) : far;
+}
+// score_in_many less `top`, in one operation less
 template <bool CAP>
 __device__ __forceinline__ float score_from(float raw, const ScoreRule& r, float top) {
     if constexpr (!CAP) return __builtin_fmaf(raw, r.scale, -top);

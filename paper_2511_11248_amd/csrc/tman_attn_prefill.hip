@@ -211,7 +211,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             for (int kb = 0; kb < kKeyBlocks; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    s[kb][i] = __builtin_fmaf(slope, (float)place(kb, i), score_of<CAP>(s[kb][i], rule));
+                    s[kb][i] = __builtin_fmaf(slope, (float)place(kb, i), score_in_many<CAP>(s[kb][i], rule));
                     best = fmaxf(best, s[kb][i]);
                 }
             best -= bias;
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
                 const uint32_t seen = PART ? seen_bits(j0 + 32 * kb, lo, hi, 4 * half) : 0;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    float x = score_of<CAP>(s[kb][i], rule);
+                    float x = score_in_many<CAP>(s[kb][i], rule);
                     if constexpr (SLOPED) x = __builtin_fmaf(-slope, fabsf(distance - (float)place(kb, i)), x);
                     if constexpr (PART) x = if_seen(x, seen, place(0, i));
                     s[kb][i] = x;
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
                 for (int i = 0; i < 16; ++i) best = fmaxf(best, s[kb][i]);
         }
         best = max_halves(best);
-        if constexpr (!PART && !SLOPED) best = score_of<CAP>(best, rule);  // a growing function of the product
+        if constexpr (!PART && !SLOPED) best = score_in_many<CAP>(best, rule);  // a growing function of the product
         // The reference of the exponentials follows the maximum only when it has fallen behind by more than kSlack: probabilities
         // then reach 2^kSlack, which both types hold as precisely as 1.
         if (__any(best > top + kSlack)) {

@@ -72,6 +72,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
     for (int x = 0; x < D / 16; ++x) q[x] = q_row[2 * x + half];
     const float slope = a.slopes ? a.slopes[r.head] * kLog2e : 0.f;
     const ScoreRule rule(a.scale, a.cap);
+    const bool sees_few = CAP && __any(r.sees && r.hi - r.lo < kFewSeen);
 
     const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
     const uint32_t mine = all + wave * kWaveBytes, k_slot = mine, v_slot = mine + kSlot;
@@ -133,9 +134,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
 
         // register i is the key at j0 + 4 half + place(i)
         auto place = [](int i) { return 8 * (i / 4) + i % 4; };
+        if constexpr (CAP) {
+            auto capped = [&](auto score) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = score(x[i], rule);
+            };
+            if (sees_few) capped(score_of<CAP>);
+            else capped(score_in_many<CAP>);
+        }
         const float distance = (float)(r.at - j0 - 4 * half);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(-slope, fabsf(distance - (float)place(i)), score_of<CAP>(x[i], rule));
+        for (int i = 0; i < 16; ++i) x[i] = __builtin_fmaf(-slope, fabsf(distance - (float)place(i)), CAP ? x[i] : score_of<CAP>(x[i], rule));
         if (part) {
             const uint32_t seen = seen_bits(j0, r.lo, r.hi, 4 * half);
 #pragma unroll

@@ -154,3 +154,37 @@ def test_bound_calls_do_what_the_calls_do():
         tman.bound_attn_decode(P.cache, attn, turned[:2], P.lens, out, 800, ws)
     with pytest.raises(tman.TmanError):
         tman.bound_rope_append(P.cache, q, k, v, P.lens, None, rope=rope)
+
+
+@pytest.mark.parametrize("sloped", [False, True])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("tokens", [0, 40, 600])  # single-token attention, few rows
+def test_capped_scores_of_single_positions(tokens, dim, sloped):
+    """A row that sees itself alone has its capped score as the logarithm of its sum: small scores as precise as large ones.
+
+    The products are exact here (one element of query and key is not zero).  Above half the cap the score has the rounding of the
+    exponential, the reciprocal and the sum, 4.3e-7 cap of at least 0.46 cap; below it some five roundings of 2^-24 and a fit of 2^-26;
+    the logarithm two more: within 2^-19 in all."""
+    n, cap = max(tokens, 1), 16.0
+    seqs = 200 if tokens == 0 else 1
+    P = Problem(dim + tokens, [n] * seqs, 4, 4, dim, 32, torch.float16, poison=0.0)
+    size = torch.exp2(torch.empty(P.k.shape[:3], device=dev()).uniform_(-9, 6, generator=P.gen))
+    sign = torch.where(torch.rand(P.k.shape[:3], generator=P.gen, device=dev()) < 0.5, -1.0, 1.0)
+    P.k.zero_()
+    P.k[..., 0] = (size * sign).half()
+    attn = tman.Attn(4, 1.0, cap=cap, window=1, slopes=P.slopes() if sloped else None)
+    rows = seqs * n
+    q = torch.zeros(rows, 4, dim, dtype=torch.float16, device=dev())
+    q[..., 0] = 1
+    out, lse = torch.empty_like(q), torch.empty(rows, 4, device=dev())
+    if tokens == 0:
+        ws = torch.zeros(max(16, tman.tman_attn_decode_workspace_bytes(P.cache, attn, n, False)), dtype=torch.uint8, device=dev())
+        tman.tman_attn_decode(P.cache, attn, q, P.lens, out, n, ws, lse=lse)
+    else:
+        ws = torch.zeros(max(16, tman.tman_attn_prefill_workspace_bytes(P.cache, attn, n, n)), dtype=torch.uint8, device=dev())
+        tman.tman_attn_prefill(P.cache, attn, q, P.ints([0, n]), P.lens, out, n, ws, lse=lse)
+    pages = P.table[:, :(n + P.page - 1) // P.page].long()
+    k = P.k[pages][..., 0].double().transpose(2, 3).reshape(seqs, -1, 4)[:, :n].reshape(rows, 4)
+    want = cap * torch.tanh(k / cap)
+    off = ((lse.double() - want) / want).abs().max().item()
+    assert off <= 2.0 ** -19, off
