@@ -182,13 +182,15 @@ def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, po
 
 
 def bound_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None, weights=None):
-    """The same, checked and marshalled once for calls that run every step with the same tensors: call(stream_handle)."""
+    """The same, checked and marshalled once for calls that run every step with the same tensors: call(stream_handle).  The call keeps
+    the tensors and handles alive."""
     where = "tman_rope_append"
     fn, args = _load().tman_rope_append, _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights)
 
     def call(stream_handle):
         _check(fn(*args, stream_handle), where)
 
+    call.holds = (cache, q, k, v, lens, q_out, rope, positions, q_start, weights)  # args are their addresses
     return call
 
 
@@ -214,13 +216,15 @@ def tman_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, wor
 
 
 def bound_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, workspace, first=None, lse=None, weights=None):
-    """The same, checked and marshalled once; max_len bounds the lengths of all the steps: call(stream_handle)."""
+    """The same, checked and marshalled once; max_len bounds the lengths of all the steps: call(stream_handle).  The call keeps the
+    tensors and handles alive."""
     where = "tman_attn_decode"
     fn, args = _load().tman_attn_decode, _decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights)
 
     def call(stream_handle):
         _check(fn(*args, stream_handle), where)
 
+    call.holds = (cache, attn, q, lens, out, workspace, first, lse, weights)  # args are their addresses
     return call
 
 
