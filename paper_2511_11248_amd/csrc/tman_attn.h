@@ -63,6 +63,7 @@ struct PrefillPlan {
     size_t partial_at, count_at, bytes;
 };
 PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len);
+size_t attn_prefill_workspace(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len);
 
 struct PrefillArgs {
     KvView c;

@@ -171,7 +171,7 @@ int tman_attn_decode(const tman_kv_cache_t* cache, const tman_attn_t* attn, cons
 size_t tman_attn_prefill_workspace_bytes(const tman_kv_cache_t* cache, const tman_attn_t* attn, int32_t n_tokens, int32_t max_len) {
     if (check_cache_sizes(cache) != TMAN_OK || check_attn(cache, attn, max_len) != TMAN_OK || n_tokens < 1) return 0;
     if (too_many_rows(n_tokens, attn->heads)) return 0;
-    return plan_attn_prefill(cache, attn, n_tokens, max_len).bytes;
+    return attn_prefill_workspace(cache, attn, n_tokens, max_len);
 }
 
 int tman_attn_prefill(const tman_kv_cache_t* cache, const tman_attn_t* attn, int32_t n_tokens, const void* q, int64_t q_stride,

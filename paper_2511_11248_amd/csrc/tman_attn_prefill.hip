@@ -508,6 +508,14 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     return p;
 }
 
+// Room for this bound and all shorter ones.  Either kernel's plan needs more for a longer bound, so what is left is a bound that goes to
+// the kernel for many rows while short ones go to the other.
+size_t attn_prefill_workspace(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len) {
+    const size_t own = plan_attn_prefill(c, a, n_tokens, max_len).bytes;
+    const size_t shorter = max_len > kShort ? plan_attn_prefill(c, a, n_tokens, kShort).bytes : 0;
+    return own > shorter ? own : shorter;
+}
+
 int launch_attn_prefill(const PrefillArgs& a, hipStream_t st) {
     const int64_t grid = (int64_t)a.p.row_tiles * a.p.n_split * a.c.kv_heads;
     if (grid > 0x7fffffff) return TMAN_ERR_SHAPE;
