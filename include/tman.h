@@ -531,7 +531,7 @@ int tman_attn_prefill(const tman_kv_cache_t *cache, const tman_attn_t *attn, int
  * keep - recent with the largest accumulated weights stay (equal weights: the lower position; NaN counts as larger than
  * all), in their order.  They are copied to the pages of new_table, with their weights; shorter sequences are copied whole.
  *   new_table : int32 [n_seqs][new_max_pages], new_max_pages * page >= keep; its pages are none that page_table uses
- *   new_lens  : int32 [n_seqs], receives min(lens[b], keep)
+ *   new_lens  : int32 [n_seqs], receives min(lens[b], keep); may be lens, must not overlap it otherwise
  *   kept      : int32 [n_seqs][kv_heads][keep], receives the kept positions, ascending (-1 behind the last of a short one)
  * Heads keep positions of their own, so afterwards a position is an index into the head's cache: distances and windows count
  * what was kept.  0 <= recent <= keep, keep >= 1, max_len as above.

@@ -249,7 +249,7 @@ def tman_attn_prefill(cache: KvCache, attn: Attn, q, q_start, lens, out, max_len
 
 def tman_kv_evict(cache: KvCache, weights, lens, keep: int, recent: int, new_table, new_lens, kept, max_len: int, stream=None) -> None:
     """Keeps `keep` positions of every sequence and key-value head (the `recent` last and the largest weights) in the pages of
-    new_table; new_lens [n_seqs] and kept [n_seqs][kv_heads][keep] receive the lengths and the positions that stayed."""
+    new_table; new_lens [n_seqs] (lens itself will do) and kept [n_seqs][kv_heads][keep] receive the lengths and the positions that stayed."""
     where = "tman_kv_evict"
     _wants(weights is not None and new_table is not None, where, _ERR_NULL)
     B = cache.n_seqs

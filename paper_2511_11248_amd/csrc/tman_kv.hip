@@ -157,7 +157,6 @@ __global__ __launch_bounds__(kSelectThreads) void evict_select_kernel(EvictArgs 
     const int hk = blockIdx.x, b = blockIdx.y;
     const int len = checked_length(a.c, a.lens, b, a.max_len);
     int32_t* kept = a.kept + ((int64_t)b * a.c.kv_heads + hk) * a.keep;
-    if (hk == 0 && threadIdx.x == 0) a.new_lens[b] = min(len, a.keep);
     if (len <= a.keep) {
         for (int r = threadIdx.x; r < a.keep; r += kSelectThreads) kept[r] = r < len ? r : -1;
         return;
@@ -301,7 +300,9 @@ template <int D>
 __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
     constexpr int kLanes = D / 8, kRows = kMoveThreads / kLanes, kEach = kRowsEach;  // lanes a row, rows at once, rows a thread
     const int hk = blockIdx.y, b = blockIdx.z;
+    // The new lengths may take the old ones' place: the choice has read those, and what is read here gives n before and after.
     const int n = min(checked_length(a.c, a.lens, b, a.max_len), a.keep);
+    if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) a.new_lens[b] = n;
     const int32_t* kept = a.kept + ((int64_t)b * a.c.kv_heads + hk) * a.keep;
     const int part = threadIdx.x % kLanes, r0 = (int)blockIdx.x * kRows * kEach + threadIdx.x / kLanes;
     int64_t from[kEach], to[kEach];

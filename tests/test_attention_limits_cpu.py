@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2511_11248_amd import attention as at
-from test_attention_abi_cpu import _attn, _cache
+from test_attention_abi_cpu import ALIGN, FAKE, SHAPE, _attn, _cache, _evict
 
 BOUNDS = (1, 31, 32, 255, 256, 257, 500, 1000, 1500, 2000, 2047, 2048, 2049, 2100, 2500, 3000, 4095, 4096, 4097, 8192, 16384, 40000, 131072, 1 << 20)
 
@@ -16,3 +16,12 @@ def test_a_prompt_workspace_for_a_longer_bound_serves_shorter_ones(dim, kv_heads
     for tokens in (1, 2, 5, 9, 33, 64, 65, 130, 200, 256, 257, 512, 700, 1000, 1024, 1500, 2048, 3001, 8192):
         need = [L.tman_attn_prefill_workspace_bytes(c, a, tokens, n) for n in BOUNDS]
         assert need == sorted(need), (tokens, need)
+
+
+def test_new_lengths_lie_in_the_place_of_the_old_ones_or_apart():
+    L, c = at._load(), _cache(n_seqs=3)
+    lens = FAKE + 64
+    for off in (-8, -4, 4, 8):
+        assert _evict(L, c, lens=lens, new=lens + off) == SHAPE
+    for off in (-12, 0, 12):
+        assert _evict(L, c, lens=lens, new=lens + off, w=FAKE + 4) == ALIGN  # not refused for where they lie
