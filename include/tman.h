@@ -534,7 +534,7 @@ int tman_attn_prefill(const tman_kv_cache_t *cache, const tman_attn_t *attn, int
  *   new_lens  : int32 [n_seqs], receives min(lens[b], keep); may be lens, must not overlap it otherwise
  *   kept      : int32 [n_seqs][kv_heads][keep], receives the kept positions, ascending (-1 behind the last of a short one)
  * Heads keep positions of their own, so afterwards a position is an index into the head's cache: distances and windows count
- * what was kept.  0 <= recent <= keep, keep >= 1, max_len as above.
+ * what was kept.  0 <= recent <= keep, 1 <= keep <= 2^30, max_len as above.
  */
 int tman_kv_evict(const tman_kv_cache_t *cache, float *weights, const int32_t *lens, int32_t keep, int32_t recent, int32_t max_len,
                   const int32_t *new_table, int32_t new_max_pages, int32_t *new_lens, int32_t *kept, void *stream);

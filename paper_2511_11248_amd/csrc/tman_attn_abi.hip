@@ -222,7 +222,7 @@ int tman_kv_evict(const tman_kv_cache_t* cache, float* weights, const int32_t* l
     const int rc = check_cache(cache);
     if (rc != TMAN_OK) return rc;
     if (!weights || !lens || !new_table || !new_lens || !kept) return TMAN_ERR_NULL;
-    if (keep < 1 || recent < 0 || recent > keep || max_len < 1 || max_len > kMostPositions) return TMAN_ERR_SHAPE;
+    if (keep < 1 || keep > kMostPositions || recent < 0 || recent > keep || max_len < 1 || max_len > kMostPositions) return TMAN_ERR_SHAPE;
     if (new_max_pages < 1 || (int64_t)new_max_pages * cache->page < keep) return TMAN_ERR_SHAPE;
     // in the place of lens, or apart from it
     if (new_lens != lens && new_lens < lens + cache->n_seqs && lens < new_lens + cache->n_seqs) return TMAN_ERR_SHAPE;

@@ -342,8 +342,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(EvictArgs a) {
 
 template <int D>
 void launch_move(const EvictArgs& a, hipStream_t st) {
-    const int rows = kMoveThreads / (D / 8) * kRowsEach;
-    evict_move_kernel<D><<<dim3((a.keep + rows - 1) / rows, a.c.kv_heads, a.c.n_seqs), kMoveThreads, 0, st>>>(a);
+    const int rows = kMoveThreads / (D / 8) * kRowsEach, most = a.keep < a.max_len ? a.keep : a.max_len;
+    evict_move_kernel<D><<<dim3((most + rows - 1) / rows, a.c.kv_heads, a.c.n_seqs), kMoveThreads, 0, st>>>(a);
 }
 
 template <class T>

@@ -25,3 +25,10 @@ def test_new_lengths_lie_in_the_place_of_the_old_ones_or_apart():
         assert _evict(L, c, lens=lens, new=lens + off) == SHAPE
     for off in (-12, 0, 12):
         assert _evict(L, c, lens=lens, new=lens + off, w=FAKE + 4) == ALIGN  # not refused for where they lie
+
+
+def test_more_is_not_kept_than_positions_can_be_numbered():
+    L, c = at._load(), _cache(page=1024)
+    for keep in ((1 << 30) + 1, (1 << 31) - 1025, (1 << 31) - 1):
+        assert _evict(L, c, keep=keep, pages=1 << 22) == SHAPE
+    assert _evict(L, c, keep=1 << 30, pages=1 << 22, w=FAKE + 4) == ALIGN  # not refused for its size
