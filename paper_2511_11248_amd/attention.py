@@ -103,7 +103,7 @@ class KvCache:
         stride, head, element = t.stride()
         if element != 1 or (head != dim and heads != 1):
             raise TmanError(_ERR_SHAPE, where)
-        return stride if tokens > 1 else max(stride, heads * dim)
+        return heads * dim if tokens == 1 else stride  # (of one token torch may keep any)
 
     def _weights(self, t, where: str) -> int:
         _wants(t.shape == self.k_pages.shape[:3] and _is(t, _float32), where)
@@ -175,7 +175,7 @@ def _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, w
 def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None, weights=None,
                      stream=None) -> None:
     """Rotates q and k (q_out may be q; both None: no queries) and writes k and v [n_tokens][kv_heads][dim] into the cache as the
-    last positions of their sequences; q_start None: one token a sequence."""
+    last positions of their sequences; q_start None: one token a sequence.  k and v have the same distance between tokens."""
     where = "tman_rope_append"
     L = _functions or _load()
     _check(L.tman_rope_append(*_append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights), _stream(stream)), where)

@@ -45,3 +45,17 @@ def test_a_bound_call_keeps_its_tensors(bind, used):
     del call
     gc.collect()
     assert [name for name, ref in alive.items() if ref() is not None] == []
+
+
+def test_a_single_token_has_no_stride():
+    """Where there is one token the distance to the next says nothing: k as a column of a fused matrix beside v of its own is taken, and so
+    is any distance that torch keeps for a dimension of one."""
+    cache = tman.KvCache(torch.zeros(8, G, PAGE, D, dtype=torch.float16), torch.zeros(8, G, PAGE, D, dtype=torch.float16),
+                         torch.zeros(1, 4, dtype=torch.int32))
+    lens = torch.zeros(1, dtype=torch.int32)
+    fused = torch.zeros(1, H + 2 * G, D, dtype=torch.float16)
+    tman.bound_rope_append(cache, fused[:, :H], fused[:, H:H + G], torch.zeros(1, G, D, dtype=torch.float16), lens, fused[:, :H])
+    odd = torch.zeros(1030, dtype=torch.float16).as_strided((1, H, D), (1030, D, 1))
+    with pytest.raises(tman.TmanError) as e:
+        tman.tman_attn_decode(cache, tman.Attn(H, 1.0), odd, lens, odd.clone(), 64, None, stream=0)
+    assert e.value.status == -5  # the workspace alone is missing
