@@ -62,6 +62,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
     for (int s = 0; s < D / 32; ++s) q[s] = q_row[4 * s + g];
     const float slope = a.slopes ? a.slopes[head] * kLog2e : 0.f;
     const ScoreRule rule(a.scale, a.cap);
+    const float below = below_largest(len - lo, kBelow);
 
     const uint32_t mine = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room) + wave * kWaveBytes;
     const uint32_t k_slot = mine, v_slot = mine + kSlot;
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
                 *reinterpret_cast<f32x4*>(to + 16) = s[1];
             }
         }
-        best = fmaxf(top, max_rows(best));
+        best = fmaxf(top, max_rows(best) - below);
         if (__any(best > top)) {
             const float f = __builtin_amdgcn_exp2f(top - best);
             sum *= f;

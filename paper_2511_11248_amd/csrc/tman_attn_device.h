@@ -173,6 +173,14 @@ __device__ __forceinline__ float score_from(float raw, const ScoreRule& r, float
     const float e = __builtin_amdgcn_exp2f(raw * r.scale);
     return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap - top);
 }
+// The reference of a row's exponentials.  The element type rounds the probabilities, and half precision has steps of 2^-24 below 2^-14: with
+// the largest at one, n small ones could lose n 2^-25 of a result, which the sum counts (131072 positions with all their weight in probabilities of
+// 2^-25.5: the whole result).  Rows that see many positions have a reference that lies powers of two below the largest score, which costs
+// no operation; where few are seen the largest probability stays one, so that the logarithm of the sum of one score is that score.
+constexpr int kLongRow = 512;
+__device__ __forceinline__ float below_largest(int seen, float most) { return seen >= kLongRow ? most : 0.f; }
+constexpr float kBelow = 14.f;  // where the reference follows the maximum at once
+
 // Rows of keys and values in LDS.  A request (one wave, 64 x 16 bytes straight into LDS) brings 1024 bytes, whole rows; lane l's 16 bytes
 // land at 16 l of it, so an arrangement that keeps the reads off each other's banks is made by choosing which bytes a lane asks for:
 // chunk c (16 bytes) of row r is kept at place c ^ key_turn(r), or c ^ value_turn(r).

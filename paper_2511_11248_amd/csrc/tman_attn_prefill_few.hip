@@ -72,6 +72,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
     for (int x = 0; x < D / 16; ++x) q[x] = q_row[2 * x + half];
     const float slope = a.slopes ? a.slopes[r.head] * kLog2e : 0.f;
     const ScoreRule rule(a.scale, a.cap);
+    const float below = below_largest(r.hi - r.lo, kBelow);
     const bool sees_few = CAP && __any(r.sees && r.hi - r.lo < kFewSeen);
 
     const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
         float best = x[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) best = fmaxf(best, x[i]);
-        best = fmaxf(top, max_halves(best));
+        best = fmaxf(top, max_halves(best) - below);
         if (__any(best > top)) {
             const float f = __builtin_amdgcn_exp2f(top - best);
             sum *= f;

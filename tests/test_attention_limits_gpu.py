@@ -38,3 +38,41 @@ def test_new_lengths_in_the_place_of_the_old_ones():
         moved = [x[b, :, :min(lens[b], keep)] for x in moved for b in range(4)]
         results.append([kept] + moved)
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("tokens", [1, 5, 150])  # single-token attention, few rows, many
+def test_many_small_probabilities_add_up(tokens, dim):
+    """Four positions of large weight, one for every wave that takes positions of its own, whose values are zero, and 131068 of exp(-17.6875) =
+    2^-25.5 of it each, whose values are one: together they are the result, 6.8e-4.
+
+    Half precision with the largest probability at one has nothing for them.  With a reference 2^7 lower at least they have steps of 2^-24 at
+    2^-18.5, so 2^-6.5 of a probability is lost at most; beside that, the rounding of the result (2^-11), what the lanes that hold the four
+    lose of the small ones in 32-bit sums (a quarter of 6.8e-4), and some 2^-11 of the sums' roundings: within 2^-6 of the result."""
+    n, seqs, peaks = 131072, 256, [0, 32, 64, 96]
+    P = Problem(71, [n], 1, 1, dim, 256, torch.float16, poison=0.0)
+    P.k.zero_()
+    P.v.fill_(1.0)
+    for j in peaks:
+        page, slot = P.row(0, j)
+        P.k[page, 0, slot, 0], P.v[page, 0, slot] = 17.6875, 0.0
+    # all sequences read the same pages: a batch that fills the chip, so that rows are not cut in pieces
+    cache, lens = tman.KvCache(P.k, P.v, P.table.repeat(seqs, 1)), P.lens.repeat(seqs)
+    rows = seqs * tokens
+    q = torch.zeros(rows, 1, dim, dtype=torch.float16, device=dev())
+    q[..., 0] = 1
+    out = torch.empty_like(q)
+    attn = tman.Attn(1, 1.0)
+    if tokens == 1:
+        ws = torch.zeros(tman.tman_attn_decode_workspace_bytes(cache, attn, n), dtype=torch.uint8, device=dev())
+        tman.tman_attn_decode(cache, attn, q, lens, out, n, ws)
+    else:
+        ws = torch.zeros(max(16, tman.tman_attn_prefill_workspace_bytes(cache, attn, rows, n)), dtype=torch.uint8, device=dev())
+        starts = torch.arange(0, rows + 1, tokens, dtype=torch.int32, device=dev())
+        tman.tman_attn_prefill(cache, attn, q, starts, lens, out, n, ws)
+    assert tman.tman_device_status() == 0
+    seen = n - tokens + 1 + torch.arange(tokens, dtype=torch.float64, device=dev())
+    small = (seen - 4) * torch.tensor(-17.6875, dtype=torch.float64).exp().item()
+    want = (small / (4 + small)).repeat(seqs)[:, None, None]
+    off = ((out.double() - want) / want).abs().max().item()
+    assert off <= 2.0 ** -6, off
