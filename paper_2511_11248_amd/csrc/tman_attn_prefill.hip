@@ -29,7 +29,8 @@ constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kMaxSplit = 64;
 static_assert(kManyRows == kWaves * 32, "a wave takes 32 rows");
 // How far the largest score may run ahead of the reference of the exponentials, in powers of two, and where a new reference lies below
-// the largest score (of rows that see many positions).
+// the largest score.  (Of all rows: telling short ones apart takes registers that heads of 256 have not, capped 16 % slower.  The logarithm of
+// the sum of a single score is off by up to 2^-21 powers of two for it, less than the products that make a score of 32-bit sums.)
 constexpr float kSlack = 15.f, kBelowLazy = 7.f;
 constexpr int kLeastTiles = 8;  // of 64 positions, of a piece
 // The order of issue in the loop over whole tiles: how many reads of LDS run ahead of the products of keys and of values, and how many
@@ -241,7 +242,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         // The reference of the exponentials follows the maximum only when it has fallen behind by more than kSlack: probabilities
         // then reach 2^kSlack, which both types hold as precisely as 1.
         if (__any(best > top + kSlack)) {
-            const float next = fmaxf(top, best - below_largest(hi - lo, kBelowLazy)), f = __builtin_amdgcn_exp2f(top - next);
+            const float next = fmaxf(top, best - kBelowLazy), f = __builtin_amdgcn_exp2f(top - next);
             sum *= f;
 #pragma unroll
             for (int d = 0; d < kBlocks; ++d) out[d] *= f;
