@@ -479,7 +479,8 @@ int tman_rope_append(const tman_kv_cache_t *cache, const tman_rope_t *rope, int3
  * How scores are made.  For a query at position i and a key at position j, of query head h and key-value head
  * h / (heads / kv_heads):
  *   s = scale * (q . k);   cap > 0: s = cap * tanh(s / cap);   slopes: s -= slopes[h] * |i - j|
- * and window > 0 hides the keys with j <= i - window.  slopes: fp32 [heads] in device memory or NULL.
+ * and window > 0 hides the keys with j <= i - window.  slopes: fp32 [heads] in device memory or NULL.  Prompts with a cap above
+ * 256 take longer (their small scores need a more precise form).
  */
 typedef struct tman_attn {
     int32_t heads; /* of queries, a multiple of kv_heads */

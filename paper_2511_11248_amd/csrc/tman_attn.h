@@ -54,6 +54,9 @@ int launch_attn_decode(const DecodeArgs& a, hipStream_t st);
 // one piece of the positions.  Few rows go to a kernel whose waves share out the positions (32 rows a workgroup, pieces meet as in
 // decoding, or in a second kernel), many to one whose waves share out the rows (128, pieces meet in a second kernel).
 constexpr int kFewRows = 32, kManyRows = 128;
+// Caps above this have their scores made with a relative error, which the kernel for many rows has no registers for: they go to the one for
+// few rows.  Up to it the absolute error of its scores, 4.3e-7 cap, is below 1.1e-4, less than half of what rounding a probability costs.
+constexpr float kLargeCap = 256.f;
 struct PrefillPlan {
     int few;
     int second;     // pieces meet in a second kernel

@@ -136,7 +136,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[u][r] = score(s[u][r], rule);
             };
-            if (len - lo < kFewSeen) capped(score_of<CAP>);
+            if (len - lo < kFewSeen || a.cap > kLargeCap) capped(score_of<CAP>);
             else capped(score_in_many<CAP>);
         }
         const bool part = j0 < lo || j0 + kTile > len;

@@ -145,9 +145,10 @@ struct ScoreRule {
     __device__ __forceinline__ ScoreRule(float s, float c)
         : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e) {}
 };
-// cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of 2^-23 cap, whatever x.  (exp2 and the reciprocal take the time of two
-// products each here, so a polynomial for small x is no faster: six products more in their place gave the same times.)  Right for
-// rows that see many positions; the kernel for many rows, which has no registers left, makes all scores so.
+// cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of up to 4.3e-7 cap, whatever x (3.5 2^-23 cap: the reciprocal 2, the sum
+// ahead of it 1, the result 1/2).  (exp2 and the reciprocal take the time of two products each here, so a polynomial for small x is no
+// faster: six products more in their place gave the same times.)  Right for rows that see many positions and caps up to kLargeCap; the
+// kernel for many rows, which has no registers left, makes all scores so.
 template <bool CAP>
 __device__ __forceinline__ float score_in_many(float raw, const ScoreRule& r) {
     if constexpr (!CAP) return raw * r.scale;
@@ -155,7 +156,8 @@ __device__ __forceinline__ float score_in_many(float raw, const ScoreRule& r) {
     return __builtin_fmaf(-2.f * r.cap, __builtin_amdgcn_rcpf(1.f + e), r.cap);
 }
 // The same with a relative error of 2^-20: a row that sees a single position has its score as the logarithm of its sum.  Where a wave
-// has no row of fewer than kFewSeen positions, that error is spread over as many scores and not worth nine operations each.  Below
+// has no row of fewer than kFewSeen positions and the cap is not large, that error is spread over as many scores and not worth nine
+// operations each.  Below
 // |x| = 1/2, cap tanh(x) = cap x (1 + z p(z)), z = (2x log2 e)^2, with p fitted to tanh here to 2^-26.
 constexpr int kFewSeen = 16;
 template <bool CAP>

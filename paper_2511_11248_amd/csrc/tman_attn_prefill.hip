@@ -486,8 +486,9 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     // The kernel for few rows reads the keys once for every 32 rows, but starts and ends sooner and fills the chip with fewer rows: it
     // takes up to 128 rows a sequence (32 heads over 8, 32 tokens at 4096: 16 us, the other 22; 40 tokens at 16384: both 41), and short
     // sequences as long as three workgroups a unit will do (256 tokens 8.9 and 12.5 us, 512 tokens 13 and 18, 1000 tokens of 4 heads 16
-    // and 25; 100 tokens at 4096 30 and 27, 200 at 16384 109 and 80).
-    p.few = rows <= 4 * kFewRows * seqs || (max_len <= kShort && (rows + seqs * (kFewRows - 1)) / kFewRows * c->kv_heads <= 3 * kUnits);
+    // and 25; 100 tokens at 4096 30 and 27, 200 at 16384 109 and 80).  Large caps go there for their precision (8192 tokens 660 -> 1180 us).
+    p.few = a->cap > kLargeCap || rows <= 4 * kFewRows * seqs ||
+            (max_len <= kShort && (rows + seqs * (kFewRows - 1)) / kFewRows * c->kv_heads <= 3 * kUnits);
     const int tile_rows = p.few ? kFewRows : kManyRows;
     // each sequence may leave one tile filled with a single row
     const int64_t tiles = (rows + seqs * (tile_rows - 1)) / tile_rows, items = tiles * c->kv_heads;

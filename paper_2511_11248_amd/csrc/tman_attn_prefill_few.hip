@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
     const float slope = a.slopes ? a.slopes[r.head] * kLog2e : 0.f;
     const ScoreRule rule(a.scale, a.cap);
     const float below = below_largest(r.hi - r.lo, kBelow);
-    const bool sees_few = CAP && __any(r.sees && r.hi - r.lo < kFewSeen);
+    const bool precise = CAP && (a.cap > kLargeCap || __any(r.sees && r.hi - r.lo < kFewSeen));
 
     const uint32_t all = (uint32_t)reinterpret_cast<uintptr_t>((lds_pointer<uint8_t>)room);
     const uint32_t mine = all + wave * kWaveBytes, k_slot = mine, v_slot = mine + kSlot;
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[i] = score(x[i], rule);
             };
-            if (sees_few) capped(score_of<CAP>);
+            if (precise) capped(score_of<CAP>);
             else capped(score_in_many<CAP>);
         }
         const float distance = (float)(r.at - j0 - 4 * half);

@@ -4,8 +4,9 @@ import pytest
 import torch
 
 import paper_2511_11248_amd as tman
+from attention_ref import attend, gather
 from gpu_helpers import dev
-from test_attention_gpu import Problem, check_prefill
+from test_attention_gpu import Problem, check_prefill, within
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +77,29 @@ def test_many_small_probabilities_add_up(tokens, dim):
     want = (small / (4 + small)).repeat(seqs)[:, None, None]
     off = ((out.double() - want) / want).abs().max().item()
     assert off <= 2.0 ** -6, off
+
+
+@pytest.mark.parametrize("cap", [300.0, 1e4, 1e7])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("tokens", [1, 30, 400])  # single-token attention, few rows, many
+def test_large_caps_leave_small_scores_alone(tokens, dim, cap):
+    """cap tanh(s / cap) with a relative error of 2^-20, so no further off than the products are (a score of `dim` products: (dim + 8) 2^-24 of the
+    sum of their sizes): the bound of scores that are not capped holds."""
+    n = 5000
+    P = Problem(73 + tokens, [n], 4, 2, dim, 64, torch.float16)
+    q = P.normal(tokens, 4, dim)
+    out, lse = torch.empty_like(q), torch.empty(tokens, 4, device=dev())
+    attn, scale = tman.Attn(4, dim ** -0.5, cap=cap), dim ** -0.5
+    if tokens == 1:
+        ws = torch.zeros(tman.tman_attn_decode_workspace_bytes(P.cache, attn, n), dtype=torch.uint8, device=dev())
+        tman.tman_attn_decode(P.cache, attn, q, P.lens, out, n, ws, lse=lse)
+    else:
+        ws = torch.zeros(max(16, tman.tman_attn_prefill_workspace_bytes(P.cache, attn, tokens, n)), dtype=torch.uint8, device=dev())
+        tman.tman_attn_prefill(P.cache, attn, q, P.ints([0, tokens]), P.lens, out, n, ws, lse=lse)
+    k, v = gather(P.k, P.table, 0, n), gather(P.v, P.table, 0, n)
+    for i in sorted({0, tokens // 3, tokens - 1}):
+        at = n - tokens + i
+        o, l, *_ = attend(q[i], k, v, at, 0, at + 1, scale, cap, None, 0, P.dtype)
+        *_, bound, l_bound, _ = attend(q[i], k, v, at, 0, at + 1, scale, 0.0, None, 0, P.dtype)
+        within(out[i], o, bound, f"out, token {i}")
+        within(lse[i], l, l_bound, f"lse, token {i}")
