@@ -142,8 +142,9 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 struct ScoreRule {
     float scale;       // scale * log2 e, capped: 2 scale log2 e / cap
     float cap;         // cap * log2 e, or 0
+    // (a factor that a tiny cap makes infinite is cut: zero times it is zero, anything else it takes to the cap)
     __device__ __forceinline__ ScoreRule(float s, float c)
-        : scale(c > 0.f ? 2.f * s * kLog2e / c : s * kLog2e), cap(c * kLog2e) {}
+        : scale(c > 0.f ? fminf(fmaxf(2.f * s * kLog2e / c, kLowest), -kLowest) : s * kLog2e), cap(c * kLog2e) {}
 };
 // cap tanh(x) = cap - 2 cap / (1 + exp(2x)): an absolute error of up to 4.3e-7 cap, whatever x (3.5 2^-23 cap: the reciprocal 2, the sum
 // ahead of it 1, the result 1/2).  (exp2 and the reciprocal take the time of two products each here, so a polynomial for small x is no

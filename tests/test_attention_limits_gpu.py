@@ -103,3 +103,24 @@ def test_large_caps_leave_small_scores_alone(tokens, dim, cap):
         *_, bound, l_bound, _ = attend(q[i], k, v, at, 0, at + 1, scale, 0.0, None, 0, P.dtype)
         within(out[i], o, bound, f"out, token {i}")
         within(lse[i], l, l_bound, f"lse, token {i}")
+
+
+@pytest.mark.parametrize("tokens", [1, 30, 400])
+def test_a_cap_of_next_to_nothing_makes_all_scores_alike(tokens):
+    """Also the score of a product of zero: the result is the mean of the values."""
+    n, H, D = 3000, 2, 64
+    P = Problem(75, [n], H, 1, D, 64, torch.float16)
+    q = P.normal(tokens, H, D)
+    q[:, 0] = 0
+    out = torch.empty_like(q)
+    attn = tman.Attn(H, 1.0, cap=1e-42)
+    ws = torch.zeros(32 << 20, dtype=torch.uint8, device=dev())
+    if tokens == 1:
+        tman.tman_attn_decode(P.cache, attn, q, P.lens, out, n, ws)
+    else:
+        tman.tman_attn_prefill(P.cache, attn, q, P.ints([0, tokens]), P.lens, out, n, ws)
+    k, v = gather(P.k, P.table, 0, n), gather(P.v, P.table, 0, n)
+    for i in sorted({0, tokens - 1}):
+        at = n - tokens + i
+        o, _, _, bound, _, _ = attend(torch.zeros_like(q[i]), k, v, at, 0, at + 1, 1.0, 0.0, None, 0, P.dtype)
+        within(out[i], o, bound, f"token {i}")
