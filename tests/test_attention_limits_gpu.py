@@ -124,3 +124,37 @@ def test_a_cap_of_next_to_nothing_makes_all_scores_alike(tokens):
         at = n - tokens + i
         o, _, _, bound, _, _ = attend(torch.zeros_like(q[i]), k, v, at, 0, at + 1, 1.0, 0.0, None, 0, P.dtype)
         within(out[i], o, bound, f"token {i}")
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_capped_scores_of_single_positions_among_many_rows(dim):
+    """What the kernel for many rows promises of a row that sees itself alone: its score to 4.3e-7 cap.
+
+    Beside it the reference below the score, the exponential's argument, the sum's logarithm (about 7) and their sum are rounded in units of
+    powers of two, 2^-21 each with the logarithm's own error: less than 2^-19 together; and lse once, 2^-24 of itself.  The bound of 2100
+    positions keeps the kernel for few rows out of it."""
+    n, cap, heads = 600, 16.0, 4
+    P = Problem(77 + dim, [n], heads, heads, dim, 32, torch.float16, poison=0.0)
+    size = torch.exp2(torch.empty(P.k.shape[:3], device=dev()).uniform_(-9, 6, generator=P.gen))
+    sign = torch.where(torch.rand(P.k.shape[:3], generator=P.gen, device=dev()) < 0.5, -1.0, 1.0)
+    P.k.zero_()
+    P.k[..., 0] = (size * sign).half()
+    attn = tman.Attn(heads, 1.0, cap=cap, window=1)
+    q = torch.zeros(n, heads, dim, dtype=torch.float16, device=dev())
+    q[..., 0] = 1
+    out, lse = torch.empty_like(q), torch.empty(n, heads, device=dev())
+    ws = torch.zeros(max(16, tman.tman_attn_prefill_workspace_bytes(P.cache, attn, n, 2100)), dtype=torch.uint8, device=dev())
+    tman.tman_attn_prefill(P.cache, attn, q, P.ints([0, n]), P.lens, out, 2100, ws, lse=lse)
+    assert tman.tman_device_status() == 0
+    k = gather(P.k, P.table, 0, n)[..., 0].t()
+    want = cap * torch.tanh(k / cap)
+    within(lse, want, 4.3e-7 * cap + 2.0 ** -19 + 2.0 ** -24 * want.abs(), "lse")
+    assert torch.equal(out, gather(P.v, P.table, 0, n).transpose(0, 1).to(out.dtype))  # the probability of a single position is one
+
+
+def test_one_long_chunk_among_sequences_of_one_token_or_none():
+    """The choice of a kernel goes by the average: here it falls on the one for few rows."""
+    new = [300] + [b % 2 for b in range(63)]
+    P = Problem(79, [5000] + [1 + 40 * b for b in range(63)], 8, 2, 64, 32, torch.float16)
+    check_prefill(P, new, rows=20)
+    check_prefill(P, new, rows=20, cap=20.0, sloped=True, window=700)
