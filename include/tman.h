@@ -520,7 +520,10 @@ int tman_attn_decode(const tman_kv_cache_t *cache, const tman_attn_t *attn, cons
  * the result infinite or NaN.
  *   workspace : at least tman_attn_prefill_workspace_bytes for the same cache, attn and n_tokens and for max_len or more (0:
  *               NULL will do); as for tman_attn_decode
- *   max_len   : no sequence is longer
+ *   max_len   : no sequence is longer.  It sizes the launch and chooses the kernel: a tight bound makes the call faster (512 tokens of 32
+ *               heads over 8: 13 us, with a bound beyond 2048 19)
+ * The choice goes by the average of new tokens a sequence: one long chunk in a batch of many sequences with one token or none is
+ * faster in a call of its own.
  */
 size_t tman_attn_prefill_workspace_bytes(const tman_kv_cache_t *cache, const tman_attn_t *attn, int32_t n_tokens, int32_t max_len);
 int tman_attn_prefill(const tman_kv_cache_t *cache, const tman_attn_t *attn, int32_t n_tokens, const void *q, int64_t q_stride,
@@ -534,6 +537,7 @@ int tman_attn_prefill(const tman_kv_cache_t *cache, const tman_attn_t *attn, int
  *   new_table : int32 [n_seqs][new_max_pages], new_max_pages * page >= keep; its pages are none that page_table uses
  *   new_lens  : int32 [n_seqs], receives min(lens[b], keep); may be lens, must not overlap it otherwise
  *   kept      : int32 [n_seqs][kv_heads][keep], receives the kept positions, ascending (-1 behind the last of a short one)
+ * Only tman_attn_decode adds to the weights: right behind a prompt those of its positions are all zero, and the lowest ones stay.
  * Heads keep positions of their own, so afterwards a position is an index into the head's cache: distances and windows count
  * what was kept.  0 <= recent <= keep, 1 <= keep <= 2^30, max_len as above.
  */

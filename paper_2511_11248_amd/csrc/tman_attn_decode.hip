@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode_kernel
             for (int d = 0; d < D / 16; ++d) out[d] *= f;
             top = best;
         }
-        u32x4 p;
+        u32x4 p;  // rounded to the type that the matrix cores take; the sum takes them as they are
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float e[4];

@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_few_k
             for (int d = 0; d < kBlocks; ++d) out[d] *= f;
             top = best;
         }
-        u32x4 p[2];  // 16 keys each
+        u32x4 p[2];  // 16 keys each, rounded to the type that the matrix cores take; the sum takes them as they are
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
             const float e0 = __builtin_amdgcn_exp2f(x[i] - top), e1 = __builtin_amdgcn_exp2f(x[i + 1] - top);
