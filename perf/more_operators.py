@@ -474,10 +474,10 @@ def _norm(s, case):
 
 
 def _exponents(largest):
-    """The least e with largest <= 448 * 2^e, biased by 127, at least 1 (448 = 7/8 * 2^9)."""
+    """The least e with largest <= 448 * 2^e, biased by 127, at least 10 (448 = 7/8 * 2^9)."""
     part, e = torch.frexp(largest)
     e = e.long() - 9 + (part > 0.875)
-    return torch.where(largest > 0, e + 127, torch.ones_like(e)).clamp(min=1)
+    return torch.where(largest > 0, e + 127, torch.zeros_like(e)).clamp(min=10)
 
 
 def _power(e):
