@@ -544,6 +544,98 @@ int tman_attn_prefill(const tman_kv_cache_t *cache, const tman_attn_t *attn, int
 int tman_kv_evict(const tman_kv_cache_t *cache, float *weights, const int32_t *lens, int32_t keep, int32_t recent, int32_t max_len,
                   const int32_t *new_table, int32_t new_max_pages, int32_t *new_lens, int32_t *kept, void *stream);
 
+/*
+ * Norms of query and key heads, ahead of the rotation (root mean square, each head of each token by itself):
+ *   x -> x / sqrt(sum x^2 / dim + eps) * w
+ *   q_weight, k_weight : fp32 [dim], or [heads][dim] and [kv_heads][dim] (per_head = 1); 16-byte aligned; NULL: ones
+ *   eps                : at least 1e-30
+ */
+typedef struct tman_head_norm {
+    const float *q_weight;
+    const float *k_weight;
+    float eps;
+    int32_t per_head;
+} tman_head_norm_t;
+
+/* tman_rope_append with the norm of queries and keys in the same pass: normed, then rotated, all in fp32, rounded once. */
+int tman_norm_rope_append(const tman_kv_cache_t *cache, const tman_head_norm_t *norm, const tman_rope_t *rope, int32_t heads,
+                          int32_t n_tokens, const void *q, int64_t q_stride, const void *k, const void *v, int64_t kv_stride,
+                          const int32_t *positions, const int32_t *q_start, const int32_t *lens, void *q_out,
+                          int64_t q_out_stride, float *weights, void *stream);
+
+/*
+ * A cache held in 8 bits: pages of e4m3 codes (four bits of exponent, three of mantissa, largest 448, no infinities), and for
+ * every block of 16 positions, key-value head, and keys or values a power of two.  A value is code * 2^(exponent - 127).
+ *   pages          : as above, k_pages and v_pages one byte an element; `type` is that of queries, new keys and values and outputs
+ *   k_exps, v_exps : uint8 [n_pages][kv_heads][page / 16], 4-byte aligned, read in aligned words of four bytes (what lies up to three
+ *                    bytes behind the last is read and not used).  n_pages * kv_heads * page / 16 at most 2^40
+ * A block's exponent is the least (10 or more) with max |x| <= 448 * 2^(exponent - 127) over the finite values written.  New positions
+ * behind older ones of their block (of the same sequence) never lower it; where they raise it the older codes are brought to
+ * the new power of two (an exact step, but for codes that become subnormal, which are rounded to nearest even).  So what a block
+ * holds depends a little on how its positions arrived.  A value that is not finite, or would not be in `type`, is held as
+ * NaN; where the block reaches the end of `type` (fp16: above 57344) the largest codes are those that still are finite in it (fp16: 61440).
+ * A code is off by at most 2^-4 of its value, or half of 2^-9 of the block's power of two.
+ */
+typedef struct tman_kv8_cache {
+    tman_kv_cache_t pages;
+    uint8_t *k_exps;
+    uint8_t *v_exps;
+} tman_kv8_cache_t;
+
+/*
+ * tman_norm_rope_append (norm NULL: tman_rope_append) for such a cache.  Keys go from fp32 to their codes with one rounding.  Blocks that
+ * new positions share with older ones must not be shared between sequences.
+ */
+int tman_kv8_append(const tman_kv8_cache_t *cache, const tman_head_norm_t *norm, const tman_rope_t *rope, int32_t heads,
+                    int32_t n_tokens, const void *q, int64_t q_stride, const void *k, const void *v, int64_t kv_stride,
+                    const int32_t *positions, const int32_t *q_start, const int32_t *lens, void *q_out, int64_t q_out_stride,
+                    void *stream);
+
+/*
+ * tman_attn_decode and tman_attn_prefill over such a cache: they read half the bytes, otherwise the same arguments, masks, results and
+ * workspace rules (a workspace may go between all four functions).  No weights are accumulated.  Prompts of many rows are
+ * attended over a copy of the sequences' values in `type`, which lies in the workspace (2 * n_seqs * max_len * kv_heads * dim
+ * elements) as long as it takes at most TMAN_KV8_COPY_BYTES; beyond that the codes are read for every 32 rows, which takes
+ * longer: a tight max_len helps.
+ */
+#define TMAN_KV8_COPY_BYTES ((size_t)16 << 30)
+size_t tman_attn_decode_kv8_workspace_bytes(const tman_kv8_cache_t *cache, const tman_attn_t *attn, int32_t max_len);
+int tman_attn_decode_kv8(const tman_kv8_cache_t *cache, const tman_attn_t *attn, const void *q, int64_t q_stride,
+                         const int32_t *lens, const int32_t *first, int32_t max_len, void *out, int64_t out_stride, float *lse,
+                         void *workspace, size_t workspace_bytes, void *stream);
+size_t tman_attn_prefill_kv8_workspace_bytes(const tman_kv8_cache_t *cache, const tman_attn_t *attn, int32_t n_tokens, int32_t max_len);
+int tman_attn_prefill_kv8(const tman_kv8_cache_t *cache, const tman_attn_t *attn, int32_t n_tokens, const void *q,
+                          int64_t q_stride, const int32_t *q_start, const int32_t *lens, const int32_t *first, const int32_t *end,
+                          int32_t max_len, void *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/*
+ * The pages of a step: what grows gets pages, what shrinks or ends gives them back, and every new token learns its place.  For
+ * caches of any kind; all on the device, so a captured graph serves changing sequences.
+ *   page_table  : int32 [n_seqs][max_pages] as in a cache; receives the new pages behind the ones that lens[b] positions use.  `page` a
+ *                 power of two from 16 to 1024, max_pages * page at most 2^30
+ *   lens, more  : int32 [n_seqs], positions before the step and tokens that come (below zero: positions that go, from the end; -lens[b]:
+ *                 the sequence ends.  Entries of pages that went stay in the table)
+ *   free_pages  : int32 [free_capacity], a stack of which the first free_left[0] are free pages.  First the pages that went are
+ *                 put on it, in the order of the sequences and of their positions, then new pages are taken from its top, in the same order
+ *   new_lens    : int32 [n_seqs], lens + more; unchanged where nothing was granted.  May be lens
+ *   new_left    : int32 [1], what the stack holds afterwards.  May be free_left
+ *   q_start     : int32 [n_seqs + 1], where the granted tokens of every sequence start, ascending from 0
+ *   slots, positions, owners : NULL, or int64 / int32 / int32 [n_tokens]: of every granted token page * `page` + position % page,
+ *                 its position and its sequence; -1 behind the last one
+ * Tokens of a sequence are granted together or not at all: not where the stack has not enough pages for this sequence and all
+ * before it that asked for pages, where the tokens asked for up to it are more than n_tokens, or where its table is too short
+ * (which tman_device_status reports).  The caller sees it in q_start.  A length that is out of range is cut to it, `more` below
+ * -lens to -lens (reported); pages that the stack has no room for are dropped, and reported.
+ *   workspace   : at least tman_kv_plan_workspace_bytes (0: NULL will do), 16-byte aligned, any content
+ * Buffers must not overlap but for the two named.  A page must not be twice in what is free and in use.
+ */
+size_t tman_kv_plan_workspace_bytes(int32_t n_seqs, int32_t n_tokens);
+int tman_kv_plan(int32_t *page_table, int32_t n_seqs, int32_t max_pages, int32_t page, const int32_t *lens, const int32_t *more,
+                 int32_t *free_pages, int32_t free_capacity, const int32_t *free_left, int32_t n_tokens, int32_t *new_lens,
+                 int32_t *new_left, int32_t *q_start, int64_t *slots, int32_t *positions, int32_t *owners, void *workspace,
+                 size_t workspace_bytes, void *stream);
+
 /* Static, human-readable name of a status code. */
 const char *tman_status_string(int status);
 

@@ -1,5 +1,5 @@
-"""ctypes binding of the key-value cache's operators (see include/tman.h): a cache in pages, the rotation and append of new
-tokens, attention of single tokens and of prompts, and eviction by accumulated weight.
+"""ctypes binding of the key-value cache's operators (see include/tman.h): a cache in pages, of 16 bits or 8, the pages of a step, the
+norm, rotation and append of new tokens, attention of single tokens and of prompts, and eviction by accumulated weight.
 
 Argument marshalling only.  Sizes and strides come from the tensors; a tensor that cannot be what the call takes (type, number of
 dimensions, heads that are not contiguous) raises ``TmanError`` before the library is called, everything else is checked there.
@@ -26,17 +26,27 @@ class _CRope(C.Structure):
                 ("sections", C.c_int32 * 3), ("interleaved", C.c_int32)]
 
 
+class _CNorm(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float), ("per_head", C.c_int32)]
+
+
+class _CCache8(C.Structure):
+    _fields_ = [("pages", _CCache), ("k_exps", C.c_void_p), ("v_exps", C.c_void_p)]
+
+
 class _CAttn(C.Structure):
     _fields_ = [("heads", C.c_int32), ("window", C.c_int32), ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p)]
 
 
 # What the checks of every call compare with, looked up once (torch is imported with the first cache, not with this module).
-_types, _int32, _float32 = {}, None, None
+_types, _int32, _int64, _float32, _uint8, _code = {}, None, None, None, None, None
 
 
 def _learn_types() -> None:
-    global _int32, _float32
+    global _int32, _int64, _float32, _uint8, _code
     import torch
+
+    _int64, _uint8, _code = torch.int64, torch.uint8, torch.float8_e4m3fn
 
     _types.update({torch.float16: TMAN_TYPE_F16, torch.bfloat16: TMAN_TYPE_BF16})
     _int32, _float32 = torch.int32, torch.float32
@@ -71,6 +81,22 @@ def _load():
         L.tman_attn_prefill.argtypes = [vp, vp, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, vp, vp, sz, vp]
         L.tman_kv_evict.restype = C.c_int
         L.tman_kv_evict.argtypes = [vp, vp, vp, i32, i32, i32, vp, i32, vp, vp, vp]
+        L.tman_norm_rope_append.restype = C.c_int
+        L.tman_norm_rope_append.argtypes = [vp, vp, vp, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, vp, vp]
+        L.tman_kv8_append.restype = C.c_int
+        L.tman_kv8_append.argtypes = [vp, vp, vp, i32, i32, vp, i64, vp, vp, i64, vp, vp, vp, vp, i64, vp]
+        L.tman_attn_decode_kv8_workspace_bytes.restype = sz
+        L.tman_attn_decode_kv8_workspace_bytes.argtypes = [vp, vp, i32]
+        L.tman_attn_decode_kv8.restype = C.c_int
+        L.tman_attn_decode_kv8.argtypes = [vp, vp, vp, i64, vp, vp, i32, vp, i64, vp, vp, sz, vp]
+        L.tman_attn_prefill_kv8_workspace_bytes.restype = sz
+        L.tman_attn_prefill_kv8_workspace_bytes.argtypes = [vp, vp, i32, i32]
+        L.tman_attn_prefill_kv8.restype = C.c_int
+        L.tman_attn_prefill_kv8.argtypes = [vp, vp, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, vp, vp, sz, vp]
+        L.tman_kv_plan_workspace_bytes.restype = sz
+        L.tman_kv_plan_workspace_bytes.argtypes = [i32, i32]
+        L.tman_kv_plan.restype = C.c_int
+        L.tman_kv_plan.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         _functions = L
     return _functions
 
@@ -108,6 +134,55 @@ class KvCache:
     def _weights(self, t, where: str) -> int:
         _wants(t.shape == self.k_pages.shape[:3] and _is(t, _float32), where)
         return t.data_ptr()
+
+
+class KvCache8(KvCache):
+    """``tman_kv8_cache_t`` over tensors: k_pages, v_pages [n_pages][kv_heads][page][dim] of e4m3 codes (float8_e4m3fn or uint8),
+    k_exps, v_exps uint8 [n_pages][kv_heads][page / 16], page_table int32 [n_seqs][max_pages]; dtype (fp16 or bf16) of queries, new
+    keys and values, and outputs.  Keeps the tensors alive; holds no state of its own."""
+
+    def __init__(self, k_pages, v_pages, k_exps, v_exps, page_table, dtype):
+        where = "KvCache8"
+        if not _types:
+            _learn_types()
+        _wants(k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.is_contiguous() and v_pages.is_contiguous(), where)
+        kind = _types.get(dtype, -1)
+        _wants(kind >= 0 and k_pages.dtype in (_code, _uint8) and v_pages.dtype in (_code, _uint8), where, _ERR_CACHE)
+        _wants(page_table.dim() == 2 and _is(page_table, _int32), where)
+        n_pages, self.kv_heads, self.page, self.dim = k_pages.shape
+        blocks = (n_pages, self.kv_heads, self.page // 16)
+        _wants(k_exps.shape == blocks and v_exps.shape == blocks and _is(k_exps, _uint8) and _is(v_exps, _uint8), where)
+        self.k_pages, self.v_pages, self.k_exps, self.v_exps, self.page_table = k_pages, v_pages, k_exps, v_exps, page_table
+        self.n_seqs, self.max_pages = page_table.shape
+        self.dtype, self.n_pages = dtype, n_pages
+        self._c = _CCache8(_CCache(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), n_pages, self.n_seqs, self.max_pages, self.kv_heads,
+                                   self.page, self.dim, kind), _ptr(k_exps), _ptr(v_exps))
+        self._ref = C.byref(self._c)
+
+
+def _of_16_bits(cache, where: str) -> None:
+    _wants(not isinstance(cache, KvCache8), where, _ERR_CACHE)
+
+
+def _of_8_bits(cache, where: str) -> None:
+    _wants(isinstance(cache, KvCache8), where, _ERR_CACHE)
+
+
+class HeadNorm:
+    """``tman_head_norm_t``: weights fp32 [dim], or [heads][dim] of queries and [kv_heads][dim] of keys, or None for ones."""
+
+    def __init__(self, q_weight, k_weight, eps: float):
+        if not _types:
+            _learn_types()
+        given = [w for w in (q_weight, k_weight) if w is not None]
+        _wants(all(w.dim() == given[0].dim() and w.dim() in (1, 2) and _is(w, _float32) for w in given), "HeadNorm")
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, eps
+        self._c = _CNorm(_ptr(q_weight), _ptr(k_weight), eps, 1 if given and given[0].dim() == 2 else 0)
+        self._ref = C.byref(self._c)
+
+    def _fits(self, heads: int, cache, where: str) -> None:
+        for w, n in ((self.q_weight, heads), (self.k_weight, cache.kv_heads)):
+            _wants(w is None or w.shape == ((n, cache.dim) if self._c.per_head else (cache.dim,)) or n == 0, where)
 
 
 class Rope:
@@ -177,6 +252,7 @@ def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, po
     """Rotates q and k (q_out may be q; both None: no queries) and writes k and v [n_tokens][kv_heads][dim] into the cache as the
     last positions of their sequences; q_start None: one token a sequence.  k and v have the same distance between tokens."""
     where = "tman_rope_append"
+    _of_16_bits(cache, where)
     L = _functions or _load()
     _check(L.tman_rope_append(*_append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights), _stream(stream)), where)
 
@@ -185,6 +261,7 @@ def bound_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, p
     """The same, checked and marshalled once for calls that run every step with the same tensors: call(stream_handle).  The call keeps
     the tensors and handles alive."""
     where = "tman_rope_append"
+    _of_16_bits(cache, where)
     fn, args = _load().tman_rope_append, _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights)
 
     def call(stream_handle):
@@ -194,7 +271,50 @@ def bound_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, p
     return call
 
 
+def _normed(args, norm, heads, cache, where):
+    """The arguments of an append with a norm ahead of the rotation."""
+    if norm is not None:
+        norm._fits(heads, cache, where)
+    return (args[0], None if norm is None else norm._ref, *args[1:])
+
+
+def tman_norm_rope_append(cache: KvCache, norm: HeadNorm, q, k, v, lens, q_out, rope: Rope = None, positions=None, q_start=None,
+                          weights=None, stream=None) -> None:
+    """tman_rope_append with the norm of query and key heads in the same pass."""
+    where = "tman_norm_rope_append"
+    _of_16_bits(cache, where)
+    _wants(norm is not None, where, _ERR_NULL)
+    L = _functions or _load()
+    args = _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights)
+    _check(L.tman_norm_rope_append(*_normed(args, norm, args[2], cache, where), _stream(stream)), where)
+
+
+def tman_kv8_append(cache: KvCache8, q, k, v, lens, q_out, norm: HeadNorm = None, rope: Rope = None, positions=None, q_start=None,
+                    stream=None) -> None:
+    """The same (norm None: without one) into a cache held in 8 bits."""
+    where = "tman_kv8_append"
+    _of_8_bits(cache, where)
+    L = _functions or _load()
+    args = _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, None)
+    _check(L.tman_kv8_append(*_normed(args[:-1], norm, args[2], cache, where), _stream(stream)), where)
+
+
+def bound_kv8_append(cache: KvCache8, q, k, v, lens, q_out, norm: HeadNorm = None, rope: Rope = None, positions=None, q_start=None):
+    """The same, checked and marshalled once: call(stream_handle).  The call keeps the tensors and handles alive."""
+    where = "tman_kv8_append"
+    _of_8_bits(cache, where)
+    args = _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, None)
+    fn, args = _load().tman_kv8_append, _normed(args[:-1], norm, args[2], cache, where)
+
+    def call(stream_handle):
+        _check(fn(*args, stream_handle), where)
+
+    call.holds = (cache, q, k, v, lens, q_out, norm, rope, positions, q_start)  # args are their addresses
+    return call
+
+
 def tman_attn_decode_workspace_bytes(cache: KvCache, attn: Attn, max_len: int, weights: bool = False) -> int:
+    _of_16_bits(cache, "tman_attn_decode_workspace_bytes")
     return int(_load().tman_attn_decode_workspace_bytes(cache._ref, attn._ref, max_len, 1 if weights else 0))
 
 
@@ -211,6 +331,7 @@ def tman_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, wor
                      stream=None) -> None:
     """Attention of one new token of every sequence over its cache; the workspace is zero-filled once by the caller."""
     where = "tman_attn_decode"
+    _of_16_bits(cache, where)
     L = _functions or _load()
     _check(L.tman_attn_decode(*_decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights), _stream(stream)), where)
 
@@ -219,6 +340,7 @@ def bound_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, wo
     """The same, checked and marshalled once; max_len bounds the lengths of all the steps: call(stream_handle).  The call keeps the
     tensors and handles alive."""
     where = "tman_attn_decode"
+    _of_16_bits(cache, where)
     fn, args = _load().tman_attn_decode, _decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights)
 
     def call(stream_handle):
@@ -228,8 +350,50 @@ def bound_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, wo
     return call
 
 
+def tman_attn_decode_kv8_workspace_bytes(cache: KvCache8, attn: Attn, max_len: int) -> int:
+    _of_8_bits(cache, "tman_attn_decode_kv8_workspace_bytes")
+    return int(_load().tman_attn_decode_kv8_workspace_bytes(cache._ref, attn._ref, max_len))
+
+
+def _decode8_args(*args):
+    a = _decode_args(*args, None)
+    return a[:10] + a[11:]  # no weights
+
+
+def tman_attn_decode_kv8(cache: KvCache8, attn: Attn, q, lens, out, max_len: int, workspace, first=None, lse=None, stream=None) -> None:
+    """tman_attn_decode over a cache held in 8 bits."""
+    where = "tman_attn_decode_kv8"
+    _of_8_bits(cache, where)
+    L = _functions or _load()
+    _check(L.tman_attn_decode_kv8(*_decode8_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse), _stream(stream)), where)
+
+
+def bound_attn_decode_kv8(cache: KvCache8, attn: Attn, q, lens, out, max_len: int, workspace, first=None, lse=None):
+    """The same, checked and marshalled once; max_len bounds the lengths of all the steps: call(stream_handle).  The call keeps the
+    tensors and handles alive."""
+    where = "tman_attn_decode_kv8"
+    _of_8_bits(cache, where)
+    fn, args = _load().tman_attn_decode_kv8, _decode8_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse)
+
+    def call(stream_handle):
+        _check(fn(*args, stream_handle), where)
+
+    call.holds = (cache, attn, q, lens, out, workspace, first, lse)  # args are their addresses
+    return call
+
+
 def tman_attn_prefill_workspace_bytes(cache: KvCache, attn: Attn, n_tokens: int, max_len: int) -> int:
+    _of_16_bits(cache, "tman_attn_prefill_workspace_bytes")
     return int(_load().tman_attn_prefill_workspace_bytes(cache._ref, attn._ref, n_tokens, max_len))
+
+
+def _prefill_args(where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse):
+    _wants(q is not None, where, _ERR_NULL)
+    n, B, H = q.shape[0], cache.n_seqs, attn.heads
+    return (cache._ref, attn._ref, n, q.data_ptr(), cache._rows(q, where, H, n), _ints(q_start, B + 1, where), _ints(lens, B, where),
+            None if first is None else _ints(first, n, where), None if end is None else _ints(end, n, where), max_len,
+            None if out is None else out.data_ptr(), cache._rows(out, where, H, n), None if lse is None else _floats(lse, n * H, where),
+            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
 
 
 def tman_attn_prefill(cache: KvCache, attn: Attn, q, q_start, lens, out, max_len: int, workspace=None, first=None, end=None, lse=None,
@@ -237,21 +401,32 @@ def tman_attn_prefill(cache: KvCache, attn: Attn, q, q_start, lens, out, max_len
     """Attention of the new tokens of prompts over the cache that holds them; token n sees positions first[n] <= j < end[n].  A tight
     max_len makes the call faster."""
     where = "tman_attn_prefill"
-    _wants(q is not None, where, _ERR_NULL)
-    n, B, H = q.shape[0], cache.n_seqs, attn.heads
+    _of_16_bits(cache, where)
     L = _functions or _load()
-    _check(L.tman_attn_prefill(cache._ref, attn._ref, n, q.data_ptr(), cache._rows(q, where, H, n), _ints(q_start, B + 1, where),
-                               _ints(lens, B, where), None if first is None else _ints(first, n, where),
-                               None if end is None else _ints(end, n, where), max_len, None if out is None else out.data_ptr(),
-                               cache._rows(out, where, H, n), None if lse is None else _floats(lse, n * H, where),
-                               None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes,
+    _check(L.tman_attn_prefill(*_prefill_args(where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse),
                                _stream(stream)), where)
+
+
+def tman_attn_prefill_kv8_workspace_bytes(cache: KvCache8, attn: Attn, n_tokens: int, max_len: int) -> int:
+    _of_8_bits(cache, "tman_attn_prefill_kv8_workspace_bytes")
+    return int(_load().tman_attn_prefill_kv8_workspace_bytes(cache._ref, attn._ref, n_tokens, max_len))
+
+
+def tman_attn_prefill_kv8(cache: KvCache8, attn: Attn, q, q_start, lens, out, max_len: int, workspace=None, first=None, end=None,
+                          lse=None, stream=None) -> None:
+    """tman_attn_prefill over a cache held in 8 bits.  A tight max_len makes the call faster, and the workspace smaller."""
+    where = "tman_attn_prefill_kv8"
+    _of_8_bits(cache, where)
+    L = _functions or _load()
+    _check(L.tman_attn_prefill_kv8(*_prefill_args(where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse),
+                                   _stream(stream)), where)
 
 
 def tman_kv_evict(cache: KvCache, weights, lens, keep: int, recent: int, new_table, new_lens, kept, max_len: int, stream=None) -> None:
     """Keeps `keep` positions of every sequence and key-value head (the `recent` last and the largest weights) in the pages of
     new_table; new_lens [n_seqs] (lens itself will do) and kept [n_seqs][kv_heads][keep] receive the lengths and the positions that stayed."""
     where = "tman_kv_evict"
+    _of_16_bits(cache, where)
     _wants(weights is not None and new_table is not None, where, _ERR_NULL)
     B = cache.n_seqs
     _wants(new_table.dim() == 2 and new_table.shape[0] == B, where)
@@ -260,3 +435,37 @@ def tman_kv_evict(cache: KvCache, weights, lens, keep: int, recent: int, new_tab
     _check(L.tman_kv_evict(cache._ref, cache._weights(weights, where), _ints(lens, B, where), keep, recent, max_len,
                            _ints(new_table, B * pages, where), pages, _ints(new_lens, B, where),
                            _ints(kept, B * cache.kv_heads * keep, where), _stream(stream)), where)
+
+
+def tman_kv_plan_workspace_bytes(n_seqs: int, n_tokens: int) -> int:
+    return int(_load().tman_kv_plan_workspace_bytes(n_seqs, n_tokens))
+
+
+def _plan_args(where, page_table, page, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots, positions, owners, workspace,
+               n_tokens):
+    if not _types:
+        _learn_types()
+    _wants(page_table is not None and free_pages is not None, where, _ERR_NULL)
+    _wants(page_table.dim() == 2 and _is(page_table, _int32) and _is(free_pages, _int32) and free_pages.dim() == 1, where)
+    B = page_table.shape[0]
+    per_token = [t for t in (slots, positions, owners) if t is not None]
+    if n_tokens is None:
+        _wants(bool(per_token), where)
+        n_tokens = per_token[0].numel()
+    _wants(all(t.numel() == n_tokens for t in per_token), where)
+    _wants(slots is None or _is(slots, _int64), where)
+    return (page_table.data_ptr(), B, page_table.shape[1], page, _ints(lens, B, where), _ints(more, B, where), free_pages.data_ptr(),
+            free_pages.shape[0], _ints(free_left, 1, where), n_tokens, _ints(new_lens, B, where), _ints(new_left, 1, where),
+            _ints(q_start, B + 1, where), None if slots is None else slots.data_ptr(),
+            None if positions is None else _ints(positions, n_tokens, where), None if owners is None else _ints(owners, n_tokens, where),
+            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
+
+
+def tman_kv_plan(page_table, page: int, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots=None, positions=None,
+                 owners=None, workspace=None, n_tokens: int = None, stream=None) -> None:
+    """Gives pages of `page` positions to the sequences that grow, takes back those of the ones that shrink, and writes the places of the
+    new tokens; n_tokens, the most that are granted, is what slots, positions and owners hold."""
+    where = "tman_kv_plan"
+    L = _functions or _load()
+    _check(L.tman_kv_plan(*_plan_args(where, page_table, page, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots,
+                                      positions, owners, workspace, n_tokens), _stream(stream)), where)

@@ -65,7 +65,7 @@ struct PrefillPlan {
     int n_slots;    // of partial sums for an item (few)
     size_t partial_at, count_at, bytes;
 };
-PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len);
+PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len, bool only_few = false);
 size_t attn_prefill_workspace(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len);
 
 struct PrefillArgs {
@@ -103,8 +103,59 @@ struct AppendArgs {
     int64_t q_stride, kv_stride, q_out_stride;
     int n_pos, rot, axes, section0, section01, interleaved;  // section01: pairs of the first two axes
     int heads, n_tokens, waves_per_token;
+    const float* q_weight;  // of norms
+    const float* k_weight;
+    float eps;
+    int per_head;
 };
-int launch_rope_append(const AppendArgs& a, hipStream_t st);
+int launch_rope_append(const AppendArgs& a, bool normed, hipStream_t st);
+
+// What a cache held in 8 bits has beside its pages.
+struct Exps {
+    uint8_t* k;
+    uint8_t* v;
+};
+struct Append8Args {
+    AppendArgs a;
+    Exps e;
+    int q_groups;      // workgroups for queries, in front of the others
+    int head_chunks;   // waves that share the key-value heads of a block
+    int items;         // blocks of 16 positions, at most
+};
+int launch_kv8_append(const AppendArgs& a, const Exps& e, bool normed, hipStream_t st);
+
+int launch_attn_decode8(const DecodeArgs& a, const Exps& e, hipStream_t st);
+int launch_attn_prefill8_few(const PrefillArgs& a, const Exps& e, hipStream_t st);
+
+// The values of sequences as a cache of its own in `to.type`, page after page of a sequence: pool and table.
+struct UnpackArgs {
+    KvView from, to;
+    Exps e;
+    const int32_t* q_start;
+    const int32_t* lens;
+    int32_t* table;
+    int max_len, n_tokens, window;
+};
+int launch_kv8_unpack(const UnpackArgs& a, hipStream_t st);
+
+struct PlanArgs {
+    int32_t* table;
+    const int32_t* lens;
+    const int32_t* more;
+    int32_t* stack;
+    const int32_t* left;
+    int32_t* new_lens;
+    int32_t* new_left;
+    int32_t* q_start;
+    int64_t* slots;
+    int32_t* positions;
+    int32_t* owners;
+    int32_t* bases;  // of every sequence: where on the stack its first new page was (large calls)
+    int* status;
+    int n_seqs, max_pages, page_shift, capacity, n_tokens;
+};
+bool kv_plan_in_one(int n_seqs, int n_tokens);
+int launch_kv_plan(const PlanArgs& a, hipStream_t st);
 
 struct EvictArgs {
     KvView c;

@@ -483,7 +483,7 @@ constexpr int kUnits = 256;
 constexpr int kShort = 2048;
 constexpr int kFewJoined = 8;  // rows a sequence that the last workgroup to arrive adds up as fast as a second kernel
 
-PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len) {
+PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len, bool only_few) {
     PrefillPlan p = {};
     const int group = a->heads / c->kv_heads;
     const int64_t rows = (int64_t)n_tokens * group, seqs = c->n_seqs < n_tokens ? c->n_seqs : n_tokens;
@@ -491,7 +491,7 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     // takes up to 128 rows a sequence (32 heads over 8, 32 tokens at 4096: 16 us, the other 22; 40 tokens at 16384: both 41), and short
     // sequences as long as three workgroups a unit will do (256 tokens 8.9 and 12.5 us, 512 tokens 13 and 18, 1000 tokens of 4 heads 16
     // and 25; 100 tokens at 4096 30 and 27, 200 at 16384 109 and 80).  Large caps go there for their precision (8192 tokens 660 -> 1180 us).
-    p.few = a->cap > kLargeCap || rows <= 4 * kFewRows * seqs ||
+    p.few = only_few || a->cap > kLargeCap || rows <= 4 * kFewRows * seqs ||
             (max_len <= kShort && (rows + seqs * (kFewRows - 1)) / kFewRows * c->kv_heads <= 3 * kUnits);
     const int tile_rows = p.few ? kFewRows : kManyRows;
     // each sequence may leave one tile filled with a single row

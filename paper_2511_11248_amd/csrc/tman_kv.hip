@@ -2,7 +2,7 @@
 // accumulated attention weight).  All of it is bound by HBM: every element is read once and written once.  The rows are stored
 // as a stream that second-level caches need not keep: 5461 tokens of 3 x 32 heads 63 -> 60 us, 4096 of 32 over 8 22.5 -> 19.5; the
 // attention that reads a few appended rows next takes as long as before (append and decode of 500 positions 9.6 and 9.9 us).
-#include "tman_attn_device.h"
+#include "tman_append_device.h"
 
 namespace tman {
 namespace {
@@ -15,115 +15,9 @@ namespace {
 // 5461 tokens of 3 x 32 heads: 60 us (271 MB, 4.5 TB/s; a large copy reaches 5.1), 4096 tokens of 32 heads over 8: 19.5 us.  Reading the next rows
 // ahead of writing the present ones is no faster (66 us); a wave that takes a sixth of a token only is slower (25.5 us), since
 // finding the token's place is a chain of reads.
-constexpr int kAppendWaves = 4;
-constexpr int kAppendRuns = 4096;  // waves that fill the chip
-
-__device__ __forceinline__ void turn_pair(float& x, float& y, float c, float s) {
-    const float a = x, b = y;
-    x = __builtin_fmaf(a, c, -(b * s));
-    y = __builtin_fmaf(a, s, b * c);
-}
-
-template <class T, int D>
+template <class T, int D, bool NORM>
 __global__ __launch_bounds__(kAppendWaves * 64) void rope_append_kernel(AppendArgs a) {
-    constexpr int kUnits = D / 16, kRows = 64 / kUnits;  // head rows a wave takes at once
-    const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
-    const int run = (int)blockIdx.x * kAppendWaves + wave, n = run / a.waves_per_token;
-    if (n >= a.n_tokens) return;
-    const int unit = lane % kUnits, sub = lane / kUnits;
-    const int G = a.c.kv_heads, rows = a.heads + 2 * G;
-
-    // the sequence that token n belongs to: the last whose tokens start at or before it
-    int b = n, start = n, stop = n + 1;
-    if (a.q_start) {
-        b = 0;
-        for (int at = 0; at < a.c.n_seqs; at += 64) {
-            const int s = at + lane < a.c.n_seqs ? a.q_start[at + lane] : 0x7fffffff;
-            const int below = __popcll(__ballot(s <= n));
-            b += below;
-            if (below < 64) break;
-        }
-        b = b > 0 ? b - 1 : 0;
-        start = scalar_load(a.q_start, b);
-        stop = scalar_load(a.q_start, b + 1);
-        if (n < start || n >= stop) return;  // a token of no sequence
-    }
-    const int len = scalar_load(a.lens, b), j = len - (stop - n);  // its position
-    const int entry = j >> a.c.page_shift;
-    bool placed = j >= 0 && entry < a.c.max_pages;
-    int id = placed ? scalar_load(a.c.table, (int64_t)b * a.c.max_pages + entry) : -1;
-    placed = placed && (unsigned)id < (unsigned)a.c.n_pages;
-    if (!placed) {
-        id = 0;
-        report_index_error(a.c.status);
-    }
-    const int slot = j & ((1 << a.c.page_shift) - 1);
-
-    // the angles of the lane's eight pairs
-    const int pair = unit * 8;
-    const bool turns = pair * 2 < a.rot;
-    float c[8], s[8];
-    if (turns) {
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const int p = pair + x, axis = (p >= a.section0) + (p >= a.section01);
-            int at = a.positions ? a.positions[(int64_t)axis * a.n_tokens + n] : j;
-            if ((unsigned)at >= (unsigned)a.n_pos) {
-                report_index_error(a.c.status);
-                at = at < 0 ? 0 : a.n_pos - 1;
-            }
-            const f32x2 cs = *reinterpret_cast<const f32x2*>(a.cos_sin + ((int64_t)at * (a.rot / 2) + p) * 2);
-            c[x] = cs.x;
-            s[x] = cs.y;
-        }
-    }
-    // where a lane's 16 elements are: two runs of eight
-    const int e0 = turns && !a.interleaved ? pair : unit * 16, e1 = turns && !a.interleaved ? a.rot / 2 + pair : unit * 16 + 8;
-
-    const int step = kRows * a.waves_per_token;
-    for (int r0 = (run - n * a.waves_per_token) * kRows; r0 < rows; r0 += step) {
-        const int r = r0 + sub;
-        if (r >= rows) continue;
-        const uint8_t* from;
-        uint8_t* to;
-        const bool value = r >= a.heads + G;
-        if (r < a.heads) {
-            from = a.q + (n * a.q_stride + (int64_t)r * D) * 2;
-            to = a.q_out + (n * a.q_out_stride + (int64_t)r * D) * 2;
-        } else {
-            if (!placed) continue;
-            const int h = value ? r - a.heads - G : r - a.heads;
-            from = (value ? a.v : a.k) + (n * a.kv_stride + (int64_t)h * D) * 2;
-            const int64_t place = (((int64_t)id * G + h) << a.c.page_shift) + slot;
-            to = (value ? a.c.v : a.c.k) + place * (D * 2);
-            if (value && a.weights && unit == 0) a.weights[place] = 0.f;
-        }
-        u32x4 x = *reinterpret_cast<const u32x4*>(from + e0 * 2), y = *reinterpret_cast<const u32x4*>(from + e1 * 2);
-        if (turns && !value) {
-            float f[16];
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                f[2 * w] = T::low(x[w]);
-                f[2 * w + 1] = T::high(x[w]);
-                f[8 + 2 * w] = T::low(y[w]);
-                f[8 + 2 * w + 1] = T::high(y[w]);
-            }
-            if (a.interleaved) {
-#pragma unroll
-                for (int p = 0; p < 8; ++p) turn_pair(f[2 * p], f[2 * p + 1], c[p], s[p]);
-            } else {
-#pragma unroll
-                for (int p = 0; p < 8; ++p) turn_pair(f[p], f[8 + p], c[p], s[p]);
-            }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                x[w] = T::pack(f[2 * w], f[2 * w + 1]);
-                y[w] = T::pack(f[8 + 2 * w], f[8 + 2 * w + 1]);
-            }
-        }
-        __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(to + e0 * 2));
-        __builtin_nontemporal_store(y, reinterpret_cast<u32x4*>(to + e1 * 2));
-    }
+    append_rows<T, D, NORM, true>(a, (int)blockIdx.x * kAppendWaves + scalar((int)threadIdx.x >> 6), threadIdx.x & 63);
 }
 
 // ---- eviction: which positions stay
@@ -346,7 +240,7 @@ void launch_move(const EvictArgs& a, hipStream_t st) {
     evict_move_kernel<D><<<dim3((most + rows - 1) / rows, a.c.kv_heads, a.c.n_seqs), kMoveThreads, 0, st>>>(a);
 }
 
-template <class T>
+template <class T, bool NORM>
 void launch_append(AppendArgs a, hipStream_t st) {
     // A wave for each 1024 / D head rows of a token where there are few tokens; finding a token's place takes longer than moving those, so
     // where there are many a wave takes more of a token.
@@ -354,16 +248,16 @@ void launch_append(AppendArgs a, hipStream_t st) {
     a.waves_per_token = a.n_tokens >= kAppendRuns ? 1 : kAppendRuns / a.n_tokens;
     if (a.waves_per_token > most) a.waves_per_token = most;
     const int grid = (int)(((int64_t)a.n_tokens * a.waves_per_token + kAppendWaves - 1) / kAppendWaves);
-    if (a.c.dim == 64) rope_append_kernel<T, 64><<<grid, kAppendWaves * 64, 0, st>>>(a);
-    else if (a.c.dim == 128) rope_append_kernel<T, 128><<<grid, kAppendWaves * 64, 0, st>>>(a);
-    else rope_append_kernel<T, 256><<<grid, kAppendWaves * 64, 0, st>>>(a);
+    if (a.c.dim == 64) rope_append_kernel<T, 64, NORM><<<grid, kAppendWaves * 64, 0, st>>>(a);
+    else if (a.c.dim == 128) rope_append_kernel<T, 128, NORM><<<grid, kAppendWaves * 64, 0, st>>>(a);
+    else rope_append_kernel<T, 256, NORM><<<grid, kAppendWaves * 64, 0, st>>>(a);
 }
 
 }  // namespace
 
-int launch_rope_append(const AppendArgs& a, hipStream_t st) {
-    if (a.c.type == TMAN_TYPE_F16) launch_append<F16>(a, st);
-    else launch_append<BF16>(a, st);
+int launch_rope_append(const AppendArgs& a, bool normed, hipStream_t st) {
+    if (a.c.type == TMAN_TYPE_F16) normed ? launch_append<F16, true>(a, st) : launch_append<F16, false>(a, st);
+    else normed ? launch_append<BF16, true>(a, st) : launch_append<BF16, false>(a, st);
     return launch_status();
 }
 
