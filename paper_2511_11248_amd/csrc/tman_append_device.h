@@ -180,7 +180,7 @@ __device__ __forceinline__ void append_rows(const AppendArgs& a, int run, int la
                 const bool query = !KV || r < a.heads;
                 const float* mine = query ? a.q_weight : a.k_weight;
                 if (mine && a.per_head) mine += (query ? r : r - a.heads) * D;
-                if (mine != weighed) {  // (queries come first: ones are the first that are needed, if at all, or set again here)
+                if (mine != weighed) {
                     if (mine) {
                         load_weights(mine, u, w);
                     } else {

@@ -46,6 +46,7 @@ struct DecodeArgs {
     float* lse2;  // log2 of the sums, for the weights
     float scale, cap;
     int heads, group, window, max_len;
+    int longest_first;  // (8 bits) workgroups take the sequences by their lengths
     DecodePlan p;
 };
 int launch_attn_decode(const DecodeArgs& a, hipStream_t st);
@@ -65,7 +66,11 @@ struct PrefillPlan {
     int n_slots;    // of partial sums for an item (few)
     size_t partial_at, count_at, bytes;
 };
-PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len, bool only_few = false);
+// What the kernel for few rows reads: 16-bit values, codes of 8 bits, or codes because there is no room for the copy that the kernel for
+// many rows takes.
+enum class PromptCache { k16Bits, kCodes, kCodesOnly };
+constexpr int kShort = 2048;  // up to this bound, prompts go to the kernel for few rows as long as it takes few rounds
+PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len, PromptCache kind = PromptCache::k16Bits);
 size_t attn_prefill_workspace(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len);
 
 struct PrefillArgs {
@@ -150,11 +155,11 @@ struct PlanArgs {
     int64_t* slots;
     int32_t* positions;
     int32_t* owners;
-    int32_t* bases;  // of every sequence: where on the stack its first new page was (large calls)
+    void* workspace;
     int* status;
     int n_seqs, max_pages, page_shift, capacity, n_tokens;
 };
-bool kv_plan_in_one(int n_seqs, int n_tokens);
+size_t kv_plan_workspace(int n_seqs, int n_tokens);
 int launch_kv_plan(const PlanArgs& a, hipStream_t st);
 
 struct EvictArgs {

@@ -5,7 +5,7 @@
 // products with a key a row and a head a column), and differs in what a tile is:
 //   * Codes go straight into LDS and become elements in registers, one instruction for two of them, which takes the block's power of
 //     two along.  The products are those of a 16-bit cache that holds these values.
-//   * A tile is TILE positions, so that a wave has as many bytes under way as with 16 bits, in products of 32.
+//   * A tile is TILE positions, in products of 32, and a workgroup four or eight waves (see launch_of).
 //   * Keys are read 16 codes at a time, so the two products that they feed take coordinates 64 y + 16 g + 0..7 and + 8..15; the
 //     queries' registers hold the same.  Values come by columns, eight positions a read, which is one operand's.
 #include "tman_attn_join.h"
@@ -14,10 +14,9 @@
 namespace tman {
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * 64;
 constexpr int kHeads = 16;  // query heads of a workgroup, at most
 constexpr int kPart = 32;   // positions of a product
+constexpr int kUnits = 256;
 
 // Arrangement of rows of D codes in LDS: chunk c (16 codes) of row r is kept at place c ^ key_turn(r), or c ^ value_turn(r).
 template <int D>
@@ -31,8 +30,21 @@ struct CodeRows {
     }
 };
 
-template <class T, int D, int TILE, bool CAP>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode8_kernel(DecodeArgs a, Exps e) {
+// Sequence number `turn` of those that start with the longest, in groups of 64.
+__device__ __forceinline__ int longest_first(const DecodeArgs& a, int turn, int lane) {
+    const int at = turn & ~63, n = min(a.c.n_seqs - at, 64);
+    constexpr int kMostKey = 0x1ffffff;
+    const int len = lane < n ? a.lens[at + lane] : 0;
+    const int key = (min(max(len, 0), kMostKey) << 6) + 63 - lane;  // no two alike
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) before += __builtin_amdgcn_readlane(key, i) > key;
+    return at + __builtin_ctzll(__ballot(before == turn - at));
+}
+
+template <class T, int D, int TILE, int kWaves, bool CAP>
+__global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void attn_decode8_kernel(DecodeArgs a, Exps e) {
+    constexpr int kThreads = kWaves * 64;
     using R = CodeRows<D>;
     constexpr int kParts = TILE / kPart, kBlocks = TILE / kBlock;
     constexpr int kSlot = TILE * D, kRequests = kSlot / 1024, kBlockRequests = kBlock * D / 1024;
@@ -43,7 +55,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode8_kerne
     __shared__ int last;
 
     const int wave = scalar((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int b = blockIdx.z, hk = (int)blockIdx.y / a.p.head_chunks, chunk = (int)blockIdx.y - hk * a.p.head_chunks;
+    const int b = a.longest_first ? longest_first(a, blockIdx.z, lane) : (int)blockIdx.z, hk = (int)blockIdx.y / a.p.head_chunks, chunk = (int)blockIdx.y - hk * a.p.head_chunks;
     const int h0 = hk * a.group + chunk * kHeads, n_heads = min(kHeads, a.group - chunk * kHeads);
     const int len = checked_length(a.c, a.lens, b, a.max_len), at = len - 1;
     int lo = a.first ? max(scalar_load(a.first, b), 0) : 0;
@@ -83,27 +95,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode8_kerne
     const uint32_t k_ask = row * D + (in_row ^ R::key_turn(row)) * 16;
     const uint32_t v_ask = row * D + (in_row ^ R::value_turn(row)) * 16;
 
-    // 16 positions never leave a page
-    struct Place {
-        int64_t block[kBlocks];
-        float k_scale[kBlocks], v_scale[kBlocks];
-    };
-    auto find = [&](int t) {
-        Place p;
+    using Place = TilePlace<kBlocks>;
+    auto find = [&](int j) { return find_tile<kBlocks>(a.c, e, b, hk, len, j); };
+    auto request = [&](const uint8_t* pool, const Place& p, int j, uint32_t slot, bool keys) {
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
-            const int j = (p0 + t * kParts) * kPart + i * kBlock, id = checked_page(a.c, b, j >> a.c.page_shift, j < len);
-            p.block[i] = row_place(a.c, id, hk, j) * D;
-            const int64_t exp = exp_place(a.c, id, hk, j & ((1 << a.c.page_shift) - 1));
-            p.k_scale[i] = load_scale(e.k, exp);
-            p.v_scale[i] = load_scale(e.v, exp);
-        }
-        return p;
-    };
-    auto request = [&](const uint8_t* pool, const Place& p, uint32_t slot, bool keys) {
-#pragma unroll
-        for (int i = 0; i < kBlocks; ++i) {
-            const u32x4 rsrc = resource(pool + p.block[i], kBlock * D);
+            const u32x4 rsrc = resource(pool + row_place(a.c, p.id[i], hk, j + i * kBlock) * D, kBlock * D);
 #pragma unroll
             for (int x = 0; x < kBlockRequests; ++x) {
                 const int first_row = i * kBlock + x * R::kRowsPerRequest;
@@ -126,15 +123,17 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode8_kerne
     int t = wave;
     Place place = {};
     if (t < t1) {
-        place = find(t);
-        request(a.c.k, place, k_slot, true);
-        request(a.c.v, place, v_slot, false);
+        const int j = (p0 + t * kParts) * kPart;
+        place = find(j);
+        request(a.c.k, place, j, k_slot, true);
+        request(a.c.v, place, j, v_slot, false);
     }
     for (; t < t1; t += kWaves) {
         const bool more = t + kWaves < t1;
         const int j0 = (p0 + t * kParts) * kPart;
         Place next = {};
-        if (more) next = find(t + kWaves);
+        const int next_j = j0 + kWaves * TILE;
+        if (more) next = find(next_j);
         wait_requests<kRequests>();  // all but the values
         f32x4 s[kBlocks];
 #pragma unroll
@@ -144,13 +143,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode8_kerne
             for (int y = 0; y < D / 64; ++y) {
                 // (the turn of rows 16 u + col is that of col: the bits that it takes are below 16)
                 u32x4 low, high;
-                codes_to_type<T>(lds_read<u32x4>(k_read + u * kBlock * D + (k_chunk ^ (4 * y)) * 16), place.k_scale[u], low, high);
+                codes_to_type<T>(lds_read<u32x4>(k_read + u * kBlock * D + (k_chunk ^ (4 * y)) * 16), place.k_scale(u), low, high);
                 s[u] = T::mfma16(low, q[2 * y], s[u]);
                 s[u] = T::mfma16(high, q[2 * y + 1], s[u]);
             }
         }
         wait_lds();  // the keys have been read
-        if (more) request(a.c.k, next, k_slot, true);
+        if (more) request(a.c.k, next, next_j, k_slot, true);
 
         if constexpr (CAP) {
             auto capped = [&](auto score) {
@@ -207,11 +206,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode8_kerne
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
                 const u32x2 c = lds_read_code_columns(v_read + i * kPart * D + (v_chunk ^ d) * 16);
-                const u32x2 v0 = Codes<T>::to_type(c.x, place.v_scale[2 * i]), v1 = Codes<T>::to_type(c.y, place.v_scale[2 * i + 1]);
+                const u32x2 v0 = Codes<T>::to_type(c.x, place.v_scale(2 * i)), v1 = Codes<T>::to_type(c.y, place.v_scale(2 * i + 1));
                 out[d] = T::mfma16(u32x4{v0.x, v0.y, v1.x, v1.y}, p[i], out[d]);
             }
         wait_lds();
-        if (more) request(a.c.v, next, v_slot, false);
+        if (more) request(a.c.v, next, next_j, v_slot, false);
         place = next;
     }
 
@@ -243,23 +242,38 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_decode8_kerne
     Meet::pieces(base, a.tickets + item * (1 + a.p.n_slots - a.p.n_split), blockIdx.x, pieces, a.p.n_split, n_heads, all, &last, finish);
 }
 
-template <class T, int D, int TILE>
+template <class T, int D, int TILE, int WAVES>
 void launch_tiles(const DecodeArgs& a, const Exps& e, dim3 grid, hipStream_t st) {
-    if (a.cap > 0.f) attn_decode8_kernel<T, D, TILE, true><<<grid, kThreads, 0, st>>>(a, e);
-    else attn_decode8_kernel<T, D, TILE, false><<<grid, kThreads, 0, st>>>(a, e);
+    if (a.cap > 0.f) attn_decode8_kernel<T, D, TILE, WAVES, true><<<grid, WAVES * 64, 0, st>>>(a, e);
+    else attn_decode8_kernel<T, D, TILE, WAVES, false><<<grid, WAVES * 64, 0, st>>>(a, e);
 }
 
+// Waves of a workgroup and positions a wave takes at once.
+//   * Where four waves have one product's positions each, that is all they take (one sequence of 777 positions 7.5 -> 6.6 us, of 100 5.5 ->
+//     4.2, against tiles of 64).
+//   * Eight waves otherwise, with 4 kB of keys and of values under way each (heads of 256: 8 kB).  Against four with twice that: 32 ragged
+//     sequences of up to 4096 104 and 108 us, 16 of up to 16384 59 and 76, 8 of up to 2000 9.4 and 10.3; heads of 64, two of 262144 103 and
+//     129; heads of 256, 16 of up to 8192 59 and 71.
+//   * Long pieces of few rows, which end together, are read faster by four waves in whole 8 kB (two sequences of 131072: 94 and 102 us);
+//     heads of 64 and 256 are not.
+constexpr int kLongPiece = 256, kManyPieces = 16;  // (in 32 positions)
 template <class T>
 void launch_of(const DecodeArgs& a, const Exps& e, dim3 grid, hipStream_t st) {
-    if (a.c.dim == 64) launch_tiles<T, 64, 128>(a, e, grid, st);
-    else if (a.c.dim == 128) launch_tiles<T, 128, 64>(a, e, grid, st);
-    else launch_tiles<T, 256, 32>(a, e, grid, st);
+    const bool one_each = a.p.split_tiles <= 4, long_pieces = a.p.split_tiles >= kLongPiece && a.p.n_split >= kManyPieces;
+    if (a.c.dim == 64) one_each ? launch_tiles<T, 64, 32, 4>(a, e, grid, st) : launch_tiles<T, 64, 64, 8>(a, e, grid, st);
+    else if (a.c.dim == 256) one_each ? launch_tiles<T, 256, 32, 4>(a, e, grid, st) : launch_tiles<T, 256, 32, 8>(a, e, grid, st);
+    else if (one_each) launch_tiles<T, 128, 32, 4>(a, e, grid, st);
+    else long_pieces ? launch_tiles<T, 128, 64, 4>(a, e, grid, st) : launch_tiles<T, 128, 32, 8>(a, e, grid, st);
 }
 
 }  // namespace
 
-int launch_attn_decode8(const DecodeArgs& a, const Exps& e, hipStream_t st) {
+int launch_attn_decode8(const DecodeArgs& args, const Exps& e, hipStream_t st) {
+    DecodeArgs a = args;
     const dim3 grid(a.p.n_split, a.c.kv_heads * a.p.head_chunks, a.c.n_seqs);
+    // Workgroups of whole rows start with the longest ones: 32 ragged sequences of up to 4096 111 -> 104 us, 64 of up to 1000 18.7 -> 17.6.
+    // Pieces of rows start together, and finding the order costs them 0.7 us.
+    a.longest_first = a.p.n_split == 1 && a.c.n_seqs > 1 && (int64_t)grid.y * grid.z > kUnits;
     if (a.c.type == TMAN_TYPE_F16) launch_of<F16>(a, e, grid, st);
     else launch_of<BF16>(a, e, grid, st);
     return launch_status();

@@ -480,10 +480,9 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 }  // namespace
 
 constexpr int kUnits = 256;
-constexpr int kShort = 2048;
 constexpr int kFewJoined = 8;  // rows a sequence that the last workgroup to arrive adds up as fast as a second kernel
 
-PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len, bool only_few) {
+PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len, PromptCache kind) {
     PrefillPlan p = {};
     const int group = a->heads / c->kv_heads;
     const int64_t rows = (int64_t)n_tokens * group, seqs = c->n_seqs < n_tokens ? c->n_seqs : n_tokens;
@@ -491,7 +490,9 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     // takes up to 128 rows a sequence (32 heads over 8, 32 tokens at 4096: 16 us, the other 22; 40 tokens at 16384: both 41), and short
     // sequences as long as three workgroups a unit will do (256 tokens 8.9 and 12.5 us, 512 tokens 13 and 18, 1000 tokens of 4 heads 16
     // and 25; 100 tokens at 4096 30 and 27, 200 at 16384 109 and 80).  Large caps go there for their precision (8192 tokens 660 -> 1180 us).
-    p.few = only_few || a->cap > kLargeCap || rows <= 4 * kFewRows * seqs ||
+    // Codes of 8 bits: up to 256 rows, since the kernel for many rows has a copy to wait for (64 tokens at 16384: 45 and 62 us, 96 tokens: 93
+    // and 70).
+    p.few = kind == PromptCache::kCodesOnly || a->cap > kLargeCap || rows <= (kind == PromptCache::k16Bits ? 4 : 8) * kFewRows * seqs ||
             (max_len <= kShort && (rows + seqs * (kFewRows - 1)) / kFewRows * c->kv_heads <= 3 * kUnits);
     const int tile_rows = p.few ? kFewRows : kManyRows;
     // each sequence may leave one tile filled with a single row
@@ -499,6 +500,12 @@ PrefillPlan plan_attn_prefill(const tman_kv_cache_t* c, const tman_attn_t* a, in
     // Few rows: a workgroup for every unit.  Many: what two workgroups a unit hold at once, and pieces of kLeastTiles tiles of what a
     // token sees in the middle of a causal prompt.
     int64_t pieces = p.few ? ceil_div(kUnits, items) : 2 * kUnits / items;  // (so there are tickets for all items that have pieces)
+    if (p.few && kind != PromptCache::k16Bits) {
+        // One workgroup of eight waves is what a unit holds, so no more than there are units, of the items there are if sequences are
+        // alike (two of 5 tokens at 16384: 26 -> 23 us, 8 of 8 at 4096: 22.4 -> 21.4).  These are half of `items` at least.
+        const int64_t likely = seqs * ceil_div(ceil_div(rows, seqs), kFewRows) * c->kv_heads;
+        pieces = kUnits / likely;
+    }
     const int64_t seen = max_len - n_tokens / seqs / 2, most = ceil_div(p.few ? max_len : seen, p.few ? 256 : kLeastTiles * 64);
     if (pieces > (p.few ? kMaxPieces : kMaxSplit)) pieces = p.few ? kMaxPieces : kMaxSplit;
     if (pieces > most) pieces = most;

@@ -11,9 +11,6 @@ namespace {
 
 constexpr int kPart = 32;  // positions of a product
 
-// Positions a wave takes at once: 8 kB of keys, as many of values.
-__host__ __device__ constexpr int tile_of(int D) { return 8192 / D; }
-
 // Arrangement of rows of D codes in LDS: chunk c (16 codes) of row r is kept at place c ^ key_turn(r), or c ^ value_turn(r).
 template <int D>
 struct CodeRows {
@@ -25,7 +22,7 @@ struct CodeRows {
         return (D == 64 ? (r >> 3) & 1 : D == 128 ? ((r >> 1) & 1) | ((r >> 2) & 2) : (r & 3) | ((r >> 1) & 4)) << 1;
     }
 };
-constexpr int kWaves = 4, kThreads = kWaves * 64;
+constexpr int kJoinThreads = 256;
 
 __device__ __forceinline__ int columns_of(const PrefillArgs& a, const RowTile& t) {  // rows of a tile
     const int64_t n = (int64_t)t.tokens * a.group - (int64_t)t.tile * kFewRows;
@@ -45,11 +42,11 @@ __device__ __forceinline__ void store_row(const PrefillArgs& a, const RowTile& t
     if (d == 0 && a.lse) a.lse[n * a.heads + head] = empty ? kMinusInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <class T, int D, bool CAP>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_kernel(PrefillArgs a, Exps e) {
+template <class T, int D, int kTile, int kWaves, bool CAP>
+__global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void attn_prefill8_few_kernel(PrefillArgs a, Exps e) {
     using R = CodeRows<D>;
     using Meet = Join<D, kFewRows, kWaves>;
-    constexpr int kTile = tile_of(D), kParts = kTile / kPart, kTileBlocks = kTile / kBlock;
+    constexpr int kParts = kTile / kPart, kTileBlocks = kTile / kBlock;
     constexpr int kSlot = kTile * D, kRequests = kSlot / 1024, kBlockRequests = kBlock * D / 1024;
     constexpr int kBlocks = D / 32;
     constexpr int kWaveBytes = 2 * kSlot > Meet::kWaveBytes ? 2 * kSlot : (Meet::kWaveBytes + 1023) / 1024 * 1024;
@@ -94,26 +91,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
     const uint32_t in_row = lane % (D / 16), row = lane / (D / 16);
     const uint32_t k_ask = row * D + (in_row ^ R::key_turn(row)) * 16;
     const uint32_t v_ask = row * D + (in_row ^ R::value_turn(row)) * 16;
-    struct Place {  // 16 positions never leave a page
-        int64_t block[kTileBlocks];
-        float k_scale[kTileBlocks], v_scale[kTileBlocks];
-    };
-    auto find = [&](int t) {
-        Place p;
+    using Place = TilePlace<kTileBlocks>;
+    auto find = [&](int j) { return find_tile<kTileBlocks>(a.c, e, b, hk, len, j); };
+    auto request = [&](const uint8_t* pool, const Place& p, int j, uint32_t slot, bool keys) {
 #pragma unroll
         for (int i = 0; i < kTileBlocks; ++i) {
-            const int j = t * kTile + i * kBlock, id = checked_page(a.c, b, j >> a.c.page_shift, j < len);
-            p.block[i] = row_place(a.c, id, hk, j) * D;
-            const int64_t exp = exp_place(a.c, id, hk, j & ((1 << a.c.page_shift) - 1));
-            p.k_scale[i] = load_scale(e.k, exp);
-            p.v_scale[i] = load_scale(e.v, exp);
-        }
-        return p;
-    };
-    auto request = [&](const uint8_t* pool, const Place& p, uint32_t slot, bool keys) {
-#pragma unroll
-        for (int i = 0; i < kTileBlocks; ++i) {
-            const u32x4 rsrc = resource(pool + p.block[i], kBlock * D);
+            const u32x4 rsrc = resource(pool + row_place(a.c, p.id[i], hk, j + i * kBlock) * D, kBlock * D);
 #pragma unroll
             for (int x = 0; x < kBlockRequests; ++x) {
                 const int first_row = i * kBlock + x * R::kRowsPerRequest;
@@ -136,22 +119,24 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
     int t = t0 + wave;
     Place place = {};
     if (t < t1) {
-        place = find(t);
-        request(a.c.k, place, k_slot, true);
-        request(a.c.v, place, v_slot, false);
+        const int j = t * kTile;
+        place = find(j);
+        request(a.c.k, place, j, k_slot, true);
+        request(a.c.v, place, j, v_slot, false);
     }
     for (; t < t1; t += kWaves) {
         const bool more = t + kWaves < t1;
         const int j0 = t * kTile;
         const bool part = j0 < inner_lo || j0 + kTile > inner_hi;
         Place next = {};
-        if (more) next = find(t + kWaves);
+        const int next_j = j0 + kWaves * kTile;
+        if (more) next = find(next_j);
         wait_requests<kRequests>();  // all but the values
         f32x16 x[kParts];
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
             x[i] = f32x16{};
-            const float scale = col < kBlock ? place.k_scale[2 * i] : place.k_scale[2 * i + 1];
+            const float scale = col < kBlock ? place.k_scale(2 * i) : place.k_scale(2 * i + 1);
 #pragma unroll
             for (int y = 0; y < D / 32; ++y) {
                 u32x4 low, high;
@@ -161,7 +146,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
             }
         }
         wait_lds();  // the keys have been read
-        if (more) request(a.c.k, next, k_slot, true);
+        if (more) request(a.c.k, next, next_j, k_slot, true);
 
         // register k of part i is the key at j0 + 4 half + at_key(i, k)
         auto at_key = [](int i, int k) { return 32 * i + 8 * (k / 4) + k % 4; };
@@ -214,7 +199,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
             for (int i = 0; i < kTileBlocks; ++i)
                 for (int y = lane; y < D; y += 64) {
                     u32x4 low, high;
-                    codes_to_type<T>(lds_read<u32x4>(v_slot + (i * D + y) * 16), place.v_scale[i], low, high);
+                    codes_to_type<T>(lds_read<u32x4>(v_slot + (i * D + y) * 16), place.v_scale(i), low, high);
                     largest = larger_bits(larger_bits(largest, low), high);
                 }
             if (__any(largest.x >= T::kExponent || largest.y >= T::kExponent)) {
@@ -227,7 +212,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 const uint32_t chunk = (2 * d + k / 2) ^ R::value_turn(y);
-                                const u32x2 w = Codes<T>::to_type(lds_read<uint32_t>(v_slot + y * D + chunk * 16 + (k & 1) * 8 + half * 4), place.v_scale[i]);
+                                const u32x2 w = Codes<T>::to_type(lds_read<uint32_t>(v_slot + y * D + chunk * 16 + (k & 1) * 8 + half * 4), place.v_scale(i));
                                 const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
                                 if (seen && (m.x & 0xffffu)) out[d][4 * k] += T::low(w.x);
                                 if (seen && (m.x >> 16)) out[d][4 * k + 1] += T::high(w.x);
@@ -240,7 +225,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
                 for (int i = 0; i < kTileBlocks; ++i)
                     for (int y = lane; y < D * 4; y += 64) {
                         const uint32_t w = lds_read<uint32_t>(v_slot + i * kBlock * D + y * 4);
-                        const u32x2 v = Codes<T>::to_type(w, place.v_scale[i]);
+                        const u32x2 v = Codes<T>::to_type(w, place.v_scale(i));
                         const u32x2 m = {not_finite<T>(v.x), not_finite<T>(v.y)};
                         lds_write(v_slot + i * kBlock * D + y * 4, w & ~((m.x & 0xffu) | (m.x >> 16 & 0xffu) << 8 | (m.y & 0xffu) << 16 | (m.y >> 16 & 0xffu) << 24));
                     }
@@ -252,11 +237,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
 #pragma unroll
             for (int d = 0; d < kBlocks; ++d) {
                 const u32x2 c = lds_read_code_columns(v_read + ks * kBlock * D + (v_chunk ^ (2 * d)) * 16);
-                const u32x2 v0 = Codes<T>::to_type(c.x, place.v_scale[ks]), v1 = Codes<T>::to_type(c.y, place.v_scale[ks]);
+                const u32x2 v0 = Codes<T>::to_type(c.x, place.v_scale(ks)), v1 = Codes<T>::to_type(c.y, place.v_scale(ks));
                 out[d] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p[ks], out[d]);
             }
         wait_lds();
-        if (more) request(a.c.v, next, v_slot, false);
+        if (more) request(a.c.v, next, next_j, v_slot, false);
         place = next;
     }
 
@@ -289,27 +274,36 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill8_few_
 
 // The pieces of an item's rows, where they are too many for one workgroup: a thread takes four coordinates of a row.
 template <class T, int D>
-__global__ __launch_bounds__(kThreads) void attn_prefill8_few_join_kernel(PrefillArgs a) {
-    using Meet = Join<D, kFewRows, kWaves>;
-    constexpr int kParts = kFewRows * (D / 4) / kThreads;
+__global__ __launch_bounds__(kJoinThreads) void attn_prefill8_few_join_kernel(PrefillArgs a) {
+    using Meet = Join<D, kFewRows, 4>;
+    constexpr int kParts = kFewRows * (D / 4) / kJoinThreads;
     const int part = (int)blockIdx.x % kParts, rest = (int)blockIdx.x / kParts, hk = rest % a.c.kv_heads, item = rest / a.c.kv_heads;
     const int64_t at = (int64_t)item * a.c.kv_heads + hk;
     const int pieces = scalar_load(a.counts, at);
     if (pieces <= 1) return;
     const RowTile rows = find_row_tile<kFewRows>(a, item, threadIdx.x & 63);
     if (rows.b < 0) return;
-    const int x = part * kThreads + threadIdx.x, c = x / (D / 4), d = x % (D / 4) * 4;
+    const int x = part * kJoinThreads + threadIdx.x, c = x / (D / 4), d = x % (D / 4) * 4;
     if (c >= columns_of(a, rows)) return;
     Meet::quad(a.partial + at * a.p.n_slots * Meet::kSlotFloats, pieces, 0, 1, c, d,
                [&](int c, int d, float m, float l, f32x4 o) { store_row<T, D>(a, rows, hk, c, d, m, l, o); });
 }
 
+// Positions a wave takes at once and waves of a workgroup.  Two sequences of 5 tokens at 16384, heads of 128: 32 positions and eight waves 26.2
+// us, 64 and eight 26.7, 64 and four 31; four of heads of 64: 29, 26, 34.  Heads of 256 have LDS for four waves' sums.
 template <class T, int D>
 void launch_of(const PrefillArgs& a, const Exps& e, int grid, hipStream_t st) {
-    auto* kernel = a.cap > 0.f ? attn_prefill8_few_kernel<T, D, true> : attn_prefill8_few_kernel<T, D, false>;
-    kernel<<<grid, kThreads, 0, st>>>(a, e);
+    constexpr int kTile = D == 64 ? 64 : 32;
+    const bool many = D == 256 || a.p.row_tiles * a.c.kv_heads > 256;
+    auto go = [&](auto waves) {
+        constexpr int kWaves = decltype(waves)::value;
+        auto* kernel = a.cap > 0.f ? attn_prefill8_few_kernel<T, D, kTile, kWaves, true> : attn_prefill8_few_kernel<T, D, kTile, kWaves, false>;
+        kernel<<<grid, kWaves * 64, 0, st>>>(a, e);
+    };
+    if (many) go(std::integral_constant<int, 4>{});
+    else go(std::integral_constant<int, D == 256 ? 4 : 8>{});
     if (a.p.second)
-        attn_prefill8_few_join_kernel<T, D><<<a.p.row_tiles * a.c.kv_heads * (kFewRows * (D / 4) / kThreads), kThreads, 0, st>>>(a);
+        attn_prefill8_few_join_kernel<T, D><<<a.p.row_tiles * a.c.kv_heads * (kFewRows * (D / 4) / kJoinThreads), kJoinThreads, 0, st>>>(a);
 }
 
 }  // namespace

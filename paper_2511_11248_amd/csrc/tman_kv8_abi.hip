@@ -30,13 +30,13 @@ struct Prefill8Plan {
 };
 Prefill8Plan plan_prefill8(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len) {
     Prefill8Plan r = {};
-    r.p = plan_attn_prefill(c, a, n_tokens, max_len);
+    r.p = plan_attn_prefill(c, a, n_tokens, max_len, PromptCache::kCodes);
     r.bytes = r.p.bytes;
     if (r.p.few) return r;
     r.seq_pages = (int)(((int64_t)max_len + c->page - 1) / c->page);
     const double values = 2.0 * c->n_seqs * r.seq_pages * c->page * c->kv_heads * c->dim;
     if (values * 2 > (double)TMAN_KV8_COPY_BYTES || (int64_t)c->n_seqs * r.seq_pages > 0x7fffffff) {
-        r.p = plan_attn_prefill(c, a, n_tokens, max_len, true);
+        r.p = plan_attn_prefill(c, a, n_tokens, max_len, PromptCache::kCodesOnly);
         r.bytes = r.p.bytes;
         return r;
     }
@@ -47,20 +47,18 @@ Prefill8Plan plan_prefill8(const tman_kv_cache_t* c, const tman_attn_t* a, int n
     return r;
 }
 
-// Room for this bound and all shorter ones.  With a shorter bound a call may go to the kernel for few rows, or the copy may fit where
-// that of a longer bound does not.
+// Room for this bound and all shorter ones.  Either kernel's plan needs more for a longer bound, so what is left are the bounds from
+// which on a call goes to the other one: short prompts, and the longest copy that fits.
 size_t prefill8_workspace(const tman_kv_cache_t* c, const tman_attn_t* a, int n_tokens, int max_len) {
     size_t most = plan_prefill8(c, a, n_tokens, max_len).bytes;
-    const size_t few = attn_prefill_workspace(c, a, n_tokens, max_len);
-    if (few > most) most = few;
-    // the longest bound whose copy fits
-    const double position = 4.0 * c->n_seqs * c->kv_heads * c->dim;
-    const double longest = (double)TMAN_KV8_COPY_BYTES / position;
-    if (longest < max_len) {
-        const int fits = (int)longest / c->page * c->page;
-        const size_t bytes = fits >= 1 ? plan_prefill8(c, a, n_tokens, fits).bytes : 0;
+    auto also = [&](double bound) {
+        if (bound < 1 || bound >= max_len) return;
+        const size_t bytes = plan_prefill8(c, a, n_tokens, (int)bound).bytes;
         if (bytes > most) most = bytes;
-    }
+    };
+    also(kShort);
+    const double longest = (double)TMAN_KV8_COPY_BYTES / (4.0 * c->n_seqs * c->kv_heads * c->dim);
+    if (longest < max_len) also((int)longest / c->page * c->page);
     return most;
 }
 
@@ -159,7 +157,7 @@ int tman_attn_prefill_kv8(const tman_kv8_cache_t* cache, const tman_attn_t* attn
 
 size_t tman_kv_plan_workspace_bytes(int32_t n_seqs, int32_t n_tokens) {
     if (n_seqs < 1 || n_seqs > kGridMost || n_tokens < 1 || n_tokens > kMostPositions) return 0;
-    return kv_plan_in_one(n_seqs, n_tokens) ? 0 : (size_t)n_seqs * sizeof(int32_t);
+    return kv_plan_workspace(n_seqs, n_tokens);
 }
 
 int tman_kv_plan(int32_t* page_table, int32_t n_seqs, int32_t max_pages, int32_t page, const int32_t* lens, const int32_t* more,
@@ -189,7 +187,7 @@ int tman_kv_plan(int32_t* page_table, int32_t n_seqs, int32_t max_pages, int32_t
     a.slots = slots;
     a.positions = positions;
     a.owners = owners;
-    a.bases = static_cast<int32_t*>(workspace);
+    a.workspace = workspace;
     a.n_seqs = n_seqs;
     a.max_pages = max_pages;
     a.page_shift = __builtin_ctz(page);

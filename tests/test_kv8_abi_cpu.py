@@ -111,7 +111,7 @@ def _plan(L, table=FAKE, B=2, pages=4, page=16, lens=FAKE, more=0x2000, stack=0x
     (dict(new=None), NULL), (dict(new_left=None), NULL), (dict(start=None), NULL), (dict(page=8), CACHE), (dict(page=24), CACHE),
     (dict(page=2048), CACHE), (dict(B=0), SHAPE), (dict(B=65536), SHAPE), (dict(pages=0), SHAPE), (dict(pages=1 << 27), SHAPE),
     (dict(cap=0), SHAPE), (dict(n=0), SHAPE), (dict(n=(1 << 30) + 1), SHAPE), (dict(new=FAKE + 4), SHAPE), (dict(slots=FAKE + 4), ALIGN),
-    (dict(n=1 << 20), WORKSPACE), (dict(n=1 << 20, ws=FAKE, wb=4), WORKSPACE), (dict(n=1 << 20, ws=FAKE + 4, wb=8), ALIGN),
+    (dict(n=1 << 20), WORKSPACE), (dict(n=1 << 20, ws=FAKE, wb=4), WORKSPACE), (dict(n=1 << 20, ws=FAKE + 4, wb=1 << 10), ALIGN),
 ])
 def test_bad_plans(over, status):
     assert _plan(at._load(), **over) == status
