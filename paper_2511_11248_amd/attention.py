@@ -177,12 +177,18 @@ class HeadNorm:
         given = [w for w in (q_weight, k_weight) if w is not None]
         _wants(all(w.dim() == given[0].dim() and w.dim() in (1, 2) and _is(w, _float32) for w in given), "HeadNorm")
         self.q_weight, self.k_weight, self.eps = q_weight, k_weight, eps
-        self._c = _CNorm(_ptr(q_weight), _ptr(k_weight), eps, 1 if given and given[0].dim() == 2 else 0)
+        per_head = bool(given) and given[0].dim() == 2
+        # what they are for, looked at once: (heads of queries or None, of keys or None, dims)
+        self._heads = tuple(w.shape[0] if per_head and w is not None else None for w in (q_weight, k_weight))
+        self._dims = {w.shape[-1] for w in given}
+        _wants(len(self._dims) <= 1, "HeadNorm")
+        self._c = _CNorm(_ptr(q_weight), _ptr(k_weight), eps, 1 if per_head else 0)
         self._ref = C.byref(self._c)
 
     def _fits(self, heads: int, cache, where: str) -> None:
-        for w, n in ((self.q_weight, heads), (self.k_weight, cache.kv_heads)):
-            _wants(w is None or w.shape == ((n, cache.dim) if self._c.per_head else (cache.dim,)) or n == 0, where)
+        q, k = self._heads
+        if (q is not None and q != heads and heads) or (k is not None and k != cache.kv_heads) or (self._dims and cache.dim not in self._dims):
+            raise TmanError(_ERR_SHAPE, where)
 
 
 class Rope:
@@ -445,20 +451,24 @@ def _plan_args(where, page_table, page, lens, more, free_pages, free_left, new_l
                n_tokens):
     if not _types:
         _learn_types()
-    _wants(page_table is not None and free_pages is not None, where, _ERR_NULL)
-    _wants(page_table.dim() == 2 and _is(page_table, _int32) and _is(free_pages, _int32) and free_pages.dim() == 1, where)
-    B = page_table.shape[0]
-    per_token = [t for t in (slots, positions, owners) if t is not None]
+    if page_table is None or free_pages is None:
+        raise TmanError(_ERR_NULL, where)
+    table, stack = page_table.shape, free_pages.shape
+    if len(table) != 2 or len(stack) != 1 or not _is(page_table, _int32) or not _is(free_pages, _int32):
+        raise TmanError(_ERR_SHAPE, where)
+    B, wide = table
     if n_tokens is None:
-        _wants(bool(per_token), where)
-        n_tokens = per_token[0].numel()
-    _wants(all(t.numel() == n_tokens for t in per_token), where)
-    _wants(slots is None or _is(slots, _int64), where)
-    return (page_table.data_ptr(), B, page_table.shape[1], page, _ints(lens, B, where), _ints(more, B, where), free_pages.data_ptr(),
-            free_pages.shape[0], _ints(free_left, 1, where), n_tokens, _ints(new_lens, B, where), _ints(new_left, 1, where),
-            _ints(q_start, B + 1, where), None if slots is None else slots.data_ptr(),
-            None if positions is None else _ints(positions, n_tokens, where), None if owners is None else _ints(owners, n_tokens, where),
-            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
+        given = slots if slots is not None else positions if positions is not None else owners
+        if given is None:
+            raise TmanError(_ERR_SHAPE, where)
+        n_tokens = given.numel()
+    if slots is not None and (slots.dtype is not _int64 or slots.numel() != n_tokens or not slots.is_contiguous()):
+        raise TmanError(_ERR_SHAPE, where)
+    return (page_table.data_ptr(), B, wide, page, _ints(lens, B, where), _ints(more, B, where), free_pages.data_ptr(), stack[0],
+            _ints(free_left, 1, where), n_tokens, _ints(new_lens, B, where), _ints(new_left, 1, where), _ints(q_start, B + 1, where),
+            None if slots is None else slots.data_ptr(), None if positions is None else _ints(positions, n_tokens, where),
+            None if owners is None else _ints(owners, n_tokens, where), None if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.nbytes)
 
 
 def tman_kv_plan(page_table, page: int, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots=None, positions=None,
@@ -469,3 +479,17 @@ def tman_kv_plan(page_table, page: int, lens, more, free_pages, free_left, new_l
     L = _functions or _load()
     _check(L.tman_kv_plan(*_plan_args(where, page_table, page, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots,
                                       positions, owners, workspace, n_tokens), _stream(stream)), where)
+
+
+def bound_kv_plan(page_table, page: int, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots=None, positions=None,
+                  owners=None, workspace=None, n_tokens: int = None):
+    """The same, checked and marshalled once: call(stream_handle).  The call keeps the tensors alive."""
+    where = "tman_kv_plan"
+    fn, args = _load().tman_kv_plan, _plan_args(where, page_table, page, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots,
+                                                positions, owners, workspace, n_tokens)
+
+    def call(stream_handle):
+        _check(fn(*args, stream_handle), where)
+
+    call.holds = (page_table, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots, positions, owners, workspace)
+    return call

@@ -123,7 +123,7 @@ struct Exps {
 struct Append8Args {
     AppendArgs a;
     Exps e;
-    int q_groups;      // workgroups for queries, in front of the others
+    int block_groups;  // workgroups for blocks, in front of those for queries
     int head_chunks;   // waves that share the key-value heads of a block
     int items;         // blocks of 16 positions, at most
 };
