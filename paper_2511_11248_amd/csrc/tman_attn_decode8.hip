@@ -96,6 +96,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
     const uint32_t v_ask = row * D + (in_row ^ R::value_turn(row)) * 16;
 
     using Place = TilePlace<kBlocks>;
+    auto find = [&](int j) { return find_tile<kBlocks>(a.c, e, b, hk, len, j); };
     auto request = [&](const uint8_t* pool, const Place& p, int j, uint32_t slot, bool keys) {
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) {
@@ -123,19 +124,16 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
     Place place = {};
     if (t < t1) {
         const int j = (p0 + t * kParts) * kPart;
-        load_pages(a.c, b, j, place);
-        check_pages(a.c, len, j, place);
+        place = find(j);
         request(a.c.k, place, j, k_slot, true);
         request(a.c.v, place, j, v_slot, false);
-        load_exps(a.c, e, hk, j, place);
     }
     for (; t < t1; t += kWaves) {
         const bool more = t + kWaves < t1;
         const int j0 = (p0 + t * kParts) * kPart;
         Place next = {};
         const int next_j = j0 + kWaves * TILE;
-        if (more) load_pages(a.c, b, next_j, next);
-        const TileScales<kBlocks> scales(a.c, hk, j0, place);
+        if (more) next = find(next_j);
         wait_requests<kRequests>();  // all but the values
         f32x4 s[kBlocks];
 #pragma unroll
@@ -145,17 +143,13 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
             for (int y = 0; y < D / 64; ++y) {
                 // (the turn of rows 16 u + col is that of col: the bits that it takes are below 16)
                 u32x4 low, high;
-                codes_to_type<T>(lds_read<u32x4>(k_read + u * kBlock * D + (k_chunk ^ (4 * y)) * 16), scales.k[u], low, high);
+                codes_to_type<T>(lds_read<u32x4>(k_read + u * kBlock * D + (k_chunk ^ (4 * y)) * 16), place.k_scale(u), low, high);
                 s[u] = T::mfma16(low, q[2 * y], s[u]);
                 s[u] = T::mfma16(high, q[2 * y + 1], s[u]);
             }
         }
         wait_lds();  // the keys have been read
-        if (more) {
-            check_pages(a.c, len, next_j, next);
-            request(a.c.k, next, next_j, k_slot, true);
-            load_exps(a.c, e, hk, next_j, next);
-        }
+        if (more) request(a.c.k, next, next_j, k_slot, true);
 
         if constexpr (CAP) {
             auto capped = [&](auto score) {
@@ -212,7 +206,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
                 const u32x2 c = lds_read_code_columns(v_read + i * kPart * D + (v_chunk ^ d) * 16);
-                const u32x2 v0 = Codes<T>::to_type(c.x, scales.v[2 * i]), v1 = Codes<T>::to_type(c.y, scales.v[2 * i + 1]);
+                const u32x2 v0 = Codes<T>::to_type(c.x, place.v_scale(2 * i)), v1 = Codes<T>::to_type(c.y, place.v_scale(2 * i + 1));
                 out[d] = T::mfma16(u32x4{v0.x, v0.y, v1.x, v1.y}, p[i], out[d]);
             }
         wait_lds();

@@ -92,6 +92,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
     const uint32_t k_ask = row * D + (in_row ^ R::key_turn(row)) * 16;
     const uint32_t v_ask = row * D + (in_row ^ R::value_turn(row)) * 16;
     using Place = TilePlace<kTileBlocks>;
+    auto find = [&](int j) { return find_tile<kTileBlocks>(a.c, e, b, hk, len, j); };
     auto request = [&](const uint8_t* pool, const Place& p, int j, uint32_t slot, bool keys) {
 #pragma unroll
         for (int i = 0; i < kTileBlocks; ++i) {
@@ -119,11 +120,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
     Place place = {};
     if (t < t1) {
         const int j = t * kTile;
-        load_pages(a.c, b, j, place);
-        check_pages(a.c, len, j, place);
+        place = find(j);
         request(a.c.k, place, j, k_slot, true);
         request(a.c.v, place, j, v_slot, false);
-        load_exps(a.c, e, hk, j, place);
     }
     for (; t < t1; t += kWaves) {
         const bool more = t + kWaves < t1;
@@ -131,14 +130,13 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
         const bool part = j0 < inner_lo || j0 + kTile > inner_hi;
         Place next = {};
         const int next_j = j0 + kWaves * kTile;
-        if (more) load_pages(a.c, b, next_j, next);
-        const TileScales<kTileBlocks> scales(a.c, hk, j0, place);
+        if (more) next = find(next_j);
         wait_requests<kRequests>();  // all but the values
         f32x16 x[kParts];
 #pragma unroll
         for (int i = 0; i < kParts; ++i) {
             x[i] = f32x16{};
-            const float scale = col < kBlock ? scales.k[2 * i] : scales.k[2 * i + 1];
+            const float scale = col < kBlock ? place.k_scale(2 * i) : place.k_scale(2 * i + 1);
 #pragma unroll
             for (int y = 0; y < D / 32; ++y) {
                 u32x4 low, high;
@@ -148,11 +146,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
             }
         }
         wait_lds();  // the keys have been read
-        if (more) {
-            check_pages(a.c, len, next_j, next);
-            request(a.c.k, next, next_j, k_slot, true);
-            load_exps(a.c, e, hk, next_j, next);
-        }
+        if (more) request(a.c.k, next, next_j, k_slot, true);
 
         // register k of part i is the key at j0 + 4 half + at_key(i, k)
         auto at_key = [](int i, int k) { return 32 * i + 8 * (k / 4) + k % 4; };
@@ -205,7 +199,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
             for (int i = 0; i < kTileBlocks; ++i)
                 for (int y = lane; y < D; y += 64) {
                     u32x4 low, high;
-                    codes_to_type<T>(lds_read<u32x4>(v_slot + (i * D + y) * 16), scales.v[i], low, high);
+                    codes_to_type<T>(lds_read<u32x4>(v_slot + (i * D + y) * 16), place.v_scale(i), low, high);
                     largest = larger_bits(larger_bits(largest, low), high);
                 }
             if (__any(largest.x >= T::kExponent || largest.y >= T::kExponent)) {
@@ -218,7 +212,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
                                 const uint32_t chunk = (2 * d + k / 2) ^ R::value_turn(y);
-                                const u32x2 w = Codes<T>::to_type(lds_read<uint32_t>(v_slot + y * D + chunk * 16 + (k & 1) * 8 + half * 4), scales.v[i]);
+                                const u32x2 w = Codes<T>::to_type(lds_read<uint32_t>(v_slot + y * D + chunk * 16 + (k & 1) * 8 + half * 4), place.v_scale(i));
                                 const u32x2 m = {not_finite<T>(w.x), not_finite<T>(w.y)};
                                 if (seen && (m.x & 0xffffu)) out[d][4 * k] += T::low(w.x);
                                 if (seen && (m.x >> 16)) out[d][4 * k + 1] += T::high(w.x);
@@ -231,7 +225,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
                 for (int i = 0; i < kTileBlocks; ++i)
                     for (int y = lane; y < D * 4; y += 64) {
                         const uint32_t w = lds_read<uint32_t>(v_slot + i * kBlock * D + y * 4);
-                        const u32x2 v = Codes<T>::to_type(w, scales.v[i]);
+                        const u32x2 v = Codes<T>::to_type(w, place.v_scale(i));
                         const u32x2 m = {not_finite<T>(v.x), not_finite<T>(v.y)};
                         lds_write(v_slot + i * kBlock * D + y * 4, w & ~((m.x & 0xffu) | (m.x >> 16 & 0xffu) << 8 | (m.y & 0xffu) << 16 | (m.y >> 16 & 0xffu) << 24));
                     }
@@ -243,7 +237,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 256 || kWaves == 8 ? 1 : 2) void 
 #pragma unroll
             for (int d = 0; d < kBlocks; ++d) {
                 const u32x2 c = lds_read_code_columns(v_read + ks * kBlock * D + (v_chunk ^ (2 * d)) * 16);
-                const u32x2 v0 = Codes<T>::to_type(c.x, scales.v[ks]), v1 = Codes<T>::to_type(c.y, scales.v[ks]);
+                const u32x2 v0 = Codes<T>::to_type(c.x, place.v_scale(ks)), v1 = Codes<T>::to_type(c.y, place.v_scale(ks));
                 out[d] = T::mfma32(u32x4{v0.x, v0.y, v1.x, v1.y}, p[ks], out[d]);
             }
         wait_lds();

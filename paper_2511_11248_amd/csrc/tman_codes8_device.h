@@ -58,22 +58,25 @@ __device__ __forceinline__ float load_scale(const uint8_t* exps, int64_t place) 
     return scale_of_exp((int)((uint32_t)load_word_of(exps, place) >> ((uint32_t)place % 4 * 8) & 255u));
 }
 
-// Where a wave's tile of N blocks from position j0 on is (16 positions never leave a page), and the words that its blocks' exponents are in.
-// Pages are asked for a step before they are needed and exponents while the codes are on their way, so neither is waited for; what is
-// kept are a few scalar registers.
+// Where a wave's tile of N blocks from position j0 on is (16 positions never leave a page), and the exponents of its blocks, a byte each: few
+// scalar registers, since the next tile's are held beside the present one's.  All pages are asked for before the first is looked at,
+// and all exponents then: two waits, however many blocks.  (Asking for pages a step ahead, and for exponents while the codes are on their
+// way, takes both waits off a wave's path and is no faster: two sequences of 131072 positions 94 -> 98 to 104 us in pages of 64 to 256
+// positions, 105 -> 98 in pages of 16, the others alike.)
 template <int N>
 struct TilePlace {
     int id[N];
-    int k_word[N], v_word[N];
+    uint32_t k_exps[(N + 3) / 4], v_exps[(N + 3) / 4];
+    __device__ __forceinline__ float k_scale(int i) const { return __builtin_bit_cast(float, (k_exps[i / 4] >> (i % 4 * 8) & 255u) << 23); }
+    __device__ __forceinline__ float v_scale(int i) const { return __builtin_bit_cast(float, (v_exps[i / 4] >> (i % 4 * 8) & 255u) << 23); }
 };
 template <int N>
-__device__ __forceinline__ void load_pages(const KvView& c, int b, int j0, TilePlace<N>& p) {
+__device__ __forceinline__ TilePlace<N> find_tile(const KvView& c, const Exps& e, int b, int hk, int len, int j0) {
+    TilePlace<N> p;
+    int k_word[N], v_word[N];
     const int32_t* row = c.table + (int64_t)b * c.max_pages;
 #pragma unroll
     for (int i = 0; i < N; ++i) p.id[i] = scalar_load(row, min((j0 + i * kBlock) >> c.page_shift, c.max_pages - 1));
-}
-template <int N>
-__device__ __forceinline__ void check_pages(const KvView& c, int len, int j0, TilePlace<N>& p) {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -81,29 +84,23 @@ __device__ __forceinline__ void check_pages(const KvView& c, int len, int j0, Ti
         bad = bad || (!inside && j0 + i * kBlock < len);
         p.id[i] = inside ? p.id[i] : 0;
     }
-    if (bad) report_index_error(c.status);
-}
-template <int N>
-__device__ __forceinline__ void load_exps(const KvView& c, const Exps& e, int hk, int j0, TilePlace<N>& p) {
+    const int in_page = (1 << c.page_shift) - 1;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int64_t at = exp_place(c, p.id[i], hk, (j0 + i * kBlock) & ((1 << c.page_shift) - 1));
-        p.k_word[i] = load_word_of(e.k, at);
-        p.v_word[i] = load_word_of(e.v, at);
+        const int64_t at = exp_place(c, p.id[i], hk, (j0 + i * kBlock) & in_page);
+        k_word[i] = load_word_of(e.k, at);
+        v_word[i] = load_word_of(e.v, at);
     }
-}
-// The powers of two of a tile's blocks, out of those words.
-template <int N>
-struct TileScales {
-    float k[N], v[N];
-    __device__ __forceinline__ TileScales(const KvView& c, int hk, int j0, const TilePlace<N>& p) {
+    if (bad) report_index_error(c.status);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const uint32_t shift = (uint32_t)exp_place(c, p.id[i], hk, (j0 + i * kBlock) & ((1 << c.page_shift) - 1)) % 4 * 8;
-            k[i] = scale_of_exp((int)((uint32_t)p.k_word[i] >> shift & 255u));
-            v[i] = scale_of_exp((int)((uint32_t)p.v_word[i] >> shift & 255u));
-        }
+    for (int i = 0; i < (N + 3) / 4; ++i) p.k_exps[i] = p.v_exps[i] = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t shift = (uint32_t)exp_place(c, p.id[i], hk, (j0 + i * kBlock) & in_page) % 4 * 8;
+        p.k_exps[i / 4] |= min((uint32_t)k_word[i] >> shift & 255u, (uint32_t)kMostExp) << (i % 4 * 8);
+        p.v_exps[i / 4] |= min((uint32_t)v_word[i] >> shift & 255u, (uint32_t)kMostExp) << (i % 4 * 8);
     }
-};
+    return p;
+}
 
 }  // namespace tman
