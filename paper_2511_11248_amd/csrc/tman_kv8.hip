@@ -27,6 +27,12 @@ __device__ __forceinline__ uint32_t largest_of_wave(uint32_t x) {
 
 __device__ __forceinline__ uint32_t bits_of(float x) { return __builtin_bit_cast(uint32_t, x); }
 
+// The largest magnitude of three: one operation, which passes over NaN.
+__device__ __forceinline__ float larger_of(float most, float a, float b) {
+    asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(most) : "v"(a), "v"(b));
+    return most;
+}
+
 // The least exponent for a largest magnitude of these bits: 448 is 1.75 * 2^8.
 __device__ __forceinline__ int exp_for(uint32_t bits) {
     return max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), kLeastExp);
@@ -150,22 +156,31 @@ __device__ __forceinline__ void append_block(const Append8Args& x, int run, int 
     };
     if (kRoomy && chunk < G) load(chunk);
     for (int h = chunk; h < G; h += x.head_chunks) {
-        float f[kPasses][16];
-        uint32_t most = 0;
+        float most_key = 0.f, f[kPasses][16], size[kPasses];  // what is held is f * size: a norm's factor is left for the last product
         if (!kRoomy) load(h);
+        u16x2 largest = {0, 0};  // of values: the bits as they came
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) to_floats<T>(lo[p], hi[p], f[p]);
+        for (int p = 0; p < kPasses; ++p) {
+            to_floats<T>(lo[p], hi[p], f[p]);
+            if (value) largest = larger_bits(larger_bits(largest, lo[p]), hi[p]);
+        }
         if (kRoomy && h + x.head_chunks < G) load(h + x.head_chunks);
         if constexpr (NORM) {
             if (!value && a.k_weight && a.per_head) load_weights(a.k_weight + (int64_t)h * D, u, w);
         }
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
+            size[p] = 1.f;
             if constexpr (NORM) {
                 if (!value) {
-                    const float inv = inverse_size<D>(f[p], a.eps);
+                    size[p] = inverse_size<D>(f[p], a.eps);
+                    if (__any(size[p] < 0x1p-60f)) {  // what a weight could take out of fp32
 #pragma unroll
-                    for (int z = 0; z < 16; ++z) f[p][z] = f[p][z] * inv * w[z];
+                        for (int z = 0; z < 16; ++z) f[p][z] *= size[p];
+                        size[p] = 1.f;
+                    }
+#pragma unroll
+                    for (int z = 0; z < 16; ++z) f[p][z] *= w[z];
                 }
             }
             if (turns && fresh[p]) {
@@ -174,20 +189,28 @@ __device__ __forceinline__ void append_block(const Append8Args& x, int run, int 
                 if (!kRoomy) load_angles(a, u, nb.first_token + j, j, c[0], s[0]);
                 turn_unit(a, f[p], c[p % kKept], s[p % kKept]);
             }
+            if (!value) {
+                float most_of_pass = 0.f;
 #pragma unroll
-            for (int z = 0; z < 16; ++z) {
-                const uint32_t m = bits_of(f[p][z]) & 0x7fffffffu;
-                most = m > most ? m : most;
+                for (int z = 0; z < 16; z += 2) {
+                    // (a signalling NaN, which bf16's bits may be, would end the maximum so far)
+                    const float x = NORM ? f[p][z] : __builtin_canonicalizef(f[p][z]), y = NORM ? f[p][z + 1] : __builtin_canonicalizef(f[p][z + 1]);
+                    most_of_pass = larger_of(most_of_pass, x, y);
+                }
+                most_key = larger_of(most_key, most_of_pass * size[p], 0.f);
             }
         }
+        uint32_t most = bits_of(value ? T::low(largest.x > largest.y ? largest.x : largest.y) : most_key);
         most = largest_of_wave(most);
-        const bool odd = most >= bits_of(Codes<T>::kInfinite);  // something is not finite: those do not count
+        // Something is not finite: it does not count.  (A key that is NaN need not come here: it is no maximum, and its code is NaN.)
+        const bool odd = most >= bits_of(Codes<T>::kInfinite);
         if (odd) {
             most = 0;
 #pragma unroll
             for (int p = 0; p < kPasses; ++p)
 #pragma unroll
                 for (int z = 0; z < 16; ++z) {
+                    f[p][z] *= size[p];
                     const uint32_t m = bits_of(f[p][z]) & 0x7fffffffu;
                     if (m < bits_of(Codes<T>::kInfinite)) most = m > most ? m : most;
                 }
@@ -218,12 +241,13 @@ __device__ __forceinline__ void append_block(const Append8Args& x, int run, int 
                 const float end = at_end ? 240.f : 448.f;
 #pragma unroll
                 for (int z = 0; z < 16; ++z) {
-                    const float y = fminf(fmaxf(f[p][z] * inv, -end), end);
-                    f[p][z] = (bits_of(f[p][z]) & 0x7fffffffu) < bits_of(Codes<T>::kInfinite) ? y : __builtin_nanf("");
+                    const float v = odd ? f[p][z] : f[p][z] * size[p], y = fminf(fmaxf(v * inv, -end), end);
+                    f[p][z] = (bits_of(v) & 0x7fffffffu) < bits_of(Codes<T>::kInfinite) ? y : __builtin_nanf("");
                 }
             } else {
+                const float factor = size[p] * inv;
 #pragma unroll
-                for (int z = 0; z < 16; ++z) f[p][z] *= inv;
+                for (int z = 0; z < 16; ++z) f[p][z] *= factor;
             }
             if (!fresh[p]) continue;
             uint8_t* row = pool + (place + p * kRows + sub) * D;

@@ -128,8 +128,10 @@ def check(C, new, rule=None, norm=None, positions=None, starts=True, q=True, mag
                     y = ref.decode(got[lo:hi].cpu()[None], torch.full((1, 1), e, dtype=torch.uint8))[0, :hi - lo] if hi - lo == 16 else \
                         got[lo:hi].cpu().view(torch.float8_e4m3fn).double() * 2.0 ** (e - 127)
                     bound = torch.maximum(part.abs() * 2.0 ** -4, torch.tensor(2.0 ** (e - 127 - 10), dtype=torch.float64))
-                    bound = bound + F32 * part.abs().amax(-1, keepdim=True)
-                    assert bool(((y - part).abs() <= bound).all())
+                    bound = bound + F32 * part.abs().nan_to_num(0.0).amax(-1, keepdim=True)
+                    nan = torch.isnan(part)
+                    assert torch.equal(torch.isnan(y), nan)
+                    assert bool(((y - part).abs() <= bound)[~nan].all())
                 got_rest, want_rest = got[n:].cpu(), want[n:]
                 assert torch.equal(got_rest, want_rest)
                 C.put(old_pages, b, h, got)
@@ -223,6 +225,40 @@ def test_ends_of_the_types(dtype):
         assert bool(torch.isfinite(rows[:, :32].to(dtype)).all()) and bool(torch.isfinite(rows[:, 64:].to(dtype)).all())
         assert bool(torch.isnan(rows[:, 48:64]).all()) and bool(torch.isnan(rows[:, 32:48, 5]).all())
         assert finite is not None and want is not None
+
+
+@pytest.mark.parametrize("dim,rule", [(64, False), (128, False), (128, True), (256, True)])
+def test_signalling_nan_beside_large_values(dim, rule):
+    """Bits of bf16 may be signalling NaN: they are held as NaN, and the others as without them."""
+    def edit(k, v):
+        for x in (k, v):
+            x[:, :, 0] = 300.0
+            bits = x.view(torch.int16)
+            bits[3, :, 1], bits[20, :, dim - 1], bits[33, 0, 2:9] = 0x7f81, -0x7f + 0x1, 0x7fa0  # 0x7f81, 0xff82, 0x7fa0
+
+    C = Cache8(6, [40], 2, 2, dim, 16, torch.bfloat16)
+    check(C, [40], edit=edit, rule=(angles(64, 16), (8,), False) if rule else None)
+
+
+def test_norms_in_an_8_bit_append_of_values_whose_squares_leave_fp32():
+    """Also where a weight would take the value itself out of fp32."""
+    C = Cache8(7, [3], 2, 1, 64, 16, torch.bfloat16)
+    w = torch.full((64,), 7.0, device=dev())
+
+    def edit(k, v):
+        k[0], k[1, :, :32], k[2] = 3e38, -2e25, 1e-3
+
+    check(C, [3], norm=tman.HeadNorm(w, w, 1e-6), edit=edit, rule=(angles(64, 64), (32,), False))
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_norms_of_rows_that_are_not_finite(dtype):
+    def edit(k, v):
+        k[3, :, 2], k[4, :, 7], k[20], k[21, :, 60] = INF, NAN, -INF, INF
+        k[22] = 0
+
+    C = Cache8(8, [30], 4, 2, 64, 16, dtype)
+    check(C, [30], edit=edit, norm=tman.HeadNorm(None, 1 + torch.rand(64, device=dev()), 1e-6), rule=(angles(64, 32), (16,), True))
 
 
 def test_growth_by_much_and_garbage_exponents():
