@@ -15,13 +15,8 @@
 //   * Only tiles in which some query of a wave does not see all keys compare positions.  There a hidden value may be anything,
 //     infinity and NaN included: such tiles are looked through, and what is not finite is left out of the products and added
 //     where it is seen.
-// Registers: heads of 128 spill 6 to 12 and heads of 256 12, outside the loop over whole tiles.  With a distance bias heads of 256 spill 39 to
-// 47, and the reloads in that loop wait for all requests under way: 8192 tokens of 16 heads over 4 650 us, with a bias 1840.  Tiles that
-// compare positions run without products beside their exponentials, and the path for values that are not finite makes them move
-// their sums from registers to registers: documents of 500 positions take 2.4 times their floor.
-// Measured and not better: 8 waves and 256 rows a workgroup (equal), tiles in a rising and a falling order (equal), issue priorities
-// (5 % slower), three workgroups a unit for heads of 64 (equal; 6 % slower on long caches).  Without the requests for keys and
-// values the loop takes 9 % less.
+// Registers: heads of 128 spill 6 to 12 and heads of 256 12 or 13, outside the loop over whole tiles.  With a distance bias and a cap heads of 256
+// spill 46, partly inside it.
 #include <type_traits>
 
 #include "tman_attn_join.h"
@@ -79,6 +74,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     constexpr int kBlocks = D / 32;
     constexpr int kBuffers = buffers_of(D), kAheadRequests = (kBuffers - 2) * 2 * kRequests;
     __shared__ __attribute__((aligned(1024))) uint8_t room[kBuffers * 2 * kSlot];
+    // Heads of 256 with a distance bias: whole tiles that lie ahead of a query are left to the loop that compares positions, since the one
+    // over whole tiles has no registers for a second form of the scores (8192 tokens of 16 heads over 4 1760 -> 1010 us, capped 1465 ->
+    // 1100).
+    constexpr bool kOnlyBehind = SLOPED && D == 256;
     __shared__ Span wave_span[kWaves];
     __shared__ __attribute__((aligned(16))) uint32_t odd_rows[kBuffers][kWaves];  // of a buffer's values: those that a wave requested are not all finite
 
@@ -210,9 +209,9 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         float best = kMinusInf;  // the largest product or score
         // Where the distance grows the score along the keys (all of them behind every query of the wave), slope * |i - j| is a
         // part of the query and a part of the key.
-        const bool behind = SLOPED && !PART && j0 + kTile - 1 <= least_at;
+        const bool behind = SLOPED && !PART && (kOnlyBehind || j0 + kTile - 1 <= least_at);
         const float bias = SLOPED ? slope * (float)(at - j0 - 4 * half) : 0.f;
-        if (SLOPED && behind) {
+        if (SLOPED && !PART && behind) {
 #pragma unroll
             for (int kb = 0; kb < kKeyBlocks; ++kb)
 #pragma unroll
@@ -221,7 +220,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
                     best = fmaxf(best, s[kb][i]);
                 }
             best -= bias;
-        } else if (PART || SLOPED) {
+        } else if (PART || (SLOPED && !kOnlyBehind)) {
             const float distance = (float)(at - j0 - 4 * half);
 #pragma unroll
             for (int kb = 0; kb < kKeyBlocks; ++kb) {
@@ -274,7 +273,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         }
         sum += more;
         bool odd_values = false;
-        if constexpr (PART) {
+        if (PART && (j0 < inner_lo || j0 + kTile > inner_hi)) {
             const u32x4 f = *reinterpret_cast<const u32x4*>(odd_rows[buffer]);
             odd_values = scalar((int)(f.x | f.y | f.z | f.w)) != 0;
         }
@@ -368,9 +367,10 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         asm volatile("" ::: "memory");
         step(t);
     };
-    // The tiles that all queries of the wave see whole are a run; before and behind it, positions are compared.  Waves pass the
-    // same number of barriers, whichever loop they are in.
-    const int whole0 = min(max((inner_lo + kTile - 1) / kTile, t0), t1), whole1 = min(max(inner_hi / kTile, whole0), t1);
+    // The tiles that all queries of the wave see whole are a run (kOnlyBehind: and that lie behind all of them); before and behind it,
+    // positions are compared.  Waves pass the same number of barriers, whichever loop they are in.
+    const int whole_hi = kOnlyBehind ? min(inner_hi - 1, least_at) + 1 : inner_hi;
+    const int whole0 = min(max((inner_lo + kTile - 1) / kTile, t0), t1), whole1 = min(max(whole_hi / kTile, whole0), t1);
     int t = t0, stop = whole0;
     auto one = [&](auto part) {
         enter(t);
