@@ -222,6 +222,16 @@ def test_prompt_rules(rule, many, dtype, dim, page):
 
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+def test_a_distance_bias_with_positions_ahead_of_the_queries(dim, cap):
+    """A prefix seen by all, also ahead of a token: whole tiles on both sides of the queries, NaN where nobody looks."""
+    lens, new = [1500, 900, 300], [1200, 900, 130]
+    end = [max(i + 1, n * 5 // 6) for n, t in zip(lens, new) for i in range(n - t, n)]
+    P = Problem8(dim + 1, lens, 4, 1, dim, 32, torch.bfloat16)
+    check_prefill(P, new, end=end, cap=cap, sloped=True, sample=range(0, 1200, 71))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
 @pytest.mark.parametrize("many", [False, True])
 def test_values_that_some_rows_must_not_see(dim, many):
     """NaN codes and blocks of overflowing exponents in places that only some rows see."""
