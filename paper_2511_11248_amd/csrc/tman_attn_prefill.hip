@@ -15,10 +15,8 @@
 //   * Only tiles in which some query of a wave does not see all keys compare positions.  There a hidden value may be anything,
 //     infinity and NaN included: such tiles are looked through, and what is not finite is left out of the products and added
 //     where it is seen.
-// Registers: heads of 128 spill 6 to 12 and heads of 256 12 or 13, outside the loop over whole tiles.  With a distance bias and a cap heads of 256
-// spill 46, partly inside it, and the reloads there wait for all requests under way.  Tiles that
-// compare positions run without products beside their exponentials, and the path for values that are not finite makes them move
-// their sums from registers to registers: documents of 500 positions take 2.4 times their floor.
+// Registers: heads of 128 with a distance bias spill 4, no others any.  Tiles that compare positions run without products beside their
+// exponentials: documents of 500 positions take 2.4 times their floor.
 // Measured and not better: 8 waves and 256 rows a workgroup (equal), tiles in a rising and a falling order (equal), issue priorities
 // (5 % slower), three workgroups a unit for heads of 64 (equal; 6 % slower on long caches).  Without the requests for keys and
 // values the loop takes 9 % less.
@@ -282,41 +280,42 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
             const u32x4 f = *reinterpret_cast<const u32x4*>(odd_rows[buffer]);
             odd_values = scalar((int)(f.x | f.y | f.z | f.w)) != 0;
         }
-        if (!PART || !odd_values) {
+        if constexpr (!PART) {
 #pragma unroll
             for (int ks = 0; ks < 2 * kKeyBlocks; ++ks)
 #pragma unroll
                 for (int d = 0; d < kBlocks; ++d) out[d] = T::mfma32(values(v_at[d & 3] + (d >> 2) * 256, ks), p[ks], out[d]);
-            if constexpr (!PART) {
-                // The order of issue: reads of LDS run ahead of the products that take them, and the vector pipe has something to do
-                // beside every product.
-                constexpr int kQk = kKeyBlocks * (D / 16), kPv = 2 * kKeyBlocks * kBlocks;
-                __builtin_amdgcn_sched_group_barrier(kReadsLds, kKeysAhead, 0);
+            // The order of issue: reads of LDS run ahead of the products that take them, and the vector pipe has something to do
+            // beside every product.
+            constexpr int kQk = kKeyBlocks * (D / 16), kPv = 2 * kKeyBlocks * kBlocks;
+            __builtin_amdgcn_sched_group_barrier(kReadsLds, kKeysAhead, 0);
 #pragma unroll
-                for (int x = 0; x < kQk; ++x) {
-                    __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kReadsLds, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kVector, kBesideKeys, 0);
-                }
-                __builtin_amdgcn_sched_group_barrier(kReadsLds, kValuesAhead, 0);
+            for (int x = 0; x < kQk; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kReadsLds, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kVector, kBesideKeys, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kReadsLds, kValuesAhead, 0);
 #pragma unroll
-                for (int x = 0; x < kPv; ++x) {
-                    __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
-                    __builtin_amdgcn_sched_group_barrier(kReadsLds, 2, 0);
-                    __builtin_amdgcn_sched_group_barrier(kVector, kBesideValues, 0);
-                }
+            for (int x = 0; x < kPv; ++x) {
+                __builtin_amdgcn_sched_group_barrier(kMatrix, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kReadsLds, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(kVector, kBesideValues, 0);
             }
         } else {
+            // (one form of the products, whether values have to be looked at or not: two would have all sums moved between them)
 #pragma unroll
             for (int ks = 0; ks < 2 * kKeyBlocks; ++ks)
 #pragma unroll
                 for (int d = 0; d < kBlocks; ++d) {
                     u32x4 v = values(v_at[d & 3] + (d >> 2) * 256, ks);
+                    if (odd_values) {
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) v[w] &= ~not_finite<T>(v[w]);
+                        for (int w = 0; w < 4; ++w) v[w] &= ~not_finite<T>(v[w]);
+                    }
                     out[d] = T::mfma32(v, p[ks], out[d]);
                 }
-            for (int y = 0; y < kTile; ++y) {
+            for (int y = 0; odd_values && y < kTile; ++y) {
                 const bool seen = j0 + y >= lo && j0 + y < hi;
 #pragma unroll
                 for (int d = 0; d < kBlocks; ++d)
