@@ -78,8 +78,8 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     constexpr int kBuffers = buffers_of(D), kAheadRequests = (kBuffers - 2) * 2 * kRequests;
     __shared__ __attribute__((aligned(1024))) uint8_t room[kBuffers * 2 * kSlot];
     // Heads of 256 with a distance bias: whole tiles that lie ahead of a query are left to the loop that compares positions, since the one
-    // over whole tiles has no registers for a second form of the scores (8192 tokens of 16 heads over 4 1760 -> 1010 us, capped 1465 ->
-    // 1100).
+    // over whole tiles has no registers for a second form of the scores (8192 tokens of 16 heads over 4, before tiles were taken from the last
+    // one down: 1760 -> 1010 us, capped 1465 -> 1100).
     constexpr bool kOnlyBehind = SLOPED && D == 256;
     __shared__ Span wave_span[kWaves];
     __shared__ __attribute__((aligned(16))) uint32_t odd_rows[kBuffers][kWaves];  // of a buffer's values: those that a wave requested are not all finite
@@ -144,8 +144,12 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     const uint32_t in_row = lane % (kRowBytes / 16), ask_row = lane / (kRowBytes / 16);
     const uint32_t k_ask = ask_row * kRowBytes + (in_row ^ R::key_turn(wave * kOwnRows + ask_row)) * 16;
     const uint32_t v_ask = ask_row * kRowBytes + (in_row ^ R::value_turn32(wave * kOwnRows + ask_row)) * 16;
+    // With a distance bias the scores of a causal row rise by up to 64 slopes a tile, so the reference would be set anew, and all sums multiplied,
+    // with nearly every tile: there the tiles are taken from the last one down (8192 tokens of 32 heads over 8 600 -> 520 us, capped 711 -> 632;
+    // heads of 256, 16 over 4, 1007 -> 702, capped 1097 -> 791).
+    auto place_of = [&](int t) { return SLOPED ? t0 + t1 - 1 - t : t; };
     auto find = [&](int t) {
-        const int j = t * kTile + wave * kOwnRows;
+        const int j = place_of(t) * kTile + wave * kOwnRows;
         return row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
     };
     // the buffers of keys, then those of values
@@ -202,7 +206,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     // wave does not see all of its keys.
     auto work_on = [&](int t, f32x16 (&s)[kKeyBlocks], f32x16 (&next_s)[kKeyBlocks], auto part) {
         constexpr bool PART = decltype(part)::value;
-        const int j0 = t * kTile;
+        const int j0 = place_of(t) * kTile;
         const uint32_t buffer = (t - t0) % kBuffers;
         uint32_t v_at[kValueReads];
 #pragma unroll
@@ -358,7 +362,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
         const int buffer = (t - t0) % kBuffers;
         if (t + kBuffers <= t1) wait_requests<kAheadRequests>();  // (the last kBuffers - 2 steps asked for all they could)
         else wait_requests<0>();
-        if (t * kTile < all_lo || (t + 1) * kTile > all_hi) {  // somebody compares positions: are all values finite?
+        if (place_of(t) * kTile < all_lo || (place_of(t) + 1) * kTile > all_hi) {  // somebody compares positions: are all values finite?
             u16x2 largest = {0, 0};
 #pragma unroll
             for (int i = 0; i < kRequests; ++i)
@@ -374,12 +378,13 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     // The tiles that all queries of the wave see whole are a run (kOnlyBehind: and that lie behind all of them); before and behind it,
     // positions are compared.  Waves pass the same number of barriers, whichever loop they are in.
     const int whole_hi = kOnlyBehind ? min(inner_hi - 1, least_at) + 1 : inner_hi;
-    const int whole0 = min(max((inner_lo + kTile - 1) / kTile, t0), t1), whole1 = min(max(whole_hi / kTile, whole0), t1);
+    const int low = min(max((inner_lo + kTile - 1) / kTile, t0), t1), high = min(max(whole_hi / kTile, low), t1);
+    const int whole0 = SLOPED ? t0 + t1 - high : low, whole1 = SLOPED ? t0 + t1 - low : high;
     int t = t0, stop = whole0;
     auto one = [&](auto part) {
         enter(t);
         if constexpr (decltype(part)::value) {
-            if (t * kTile < most && (t + 1) * kTile > least) work_on(t, s0, s0, part);
+            if (place_of(t) * kTile < most && (place_of(t) + 1) * kTile > least) work_on(t, s0, s0, part);
             products((uint32_t)(t + 1 - t0) % kBuffers, s0);
         } else {
             work_on(t, s0, s1, part);
