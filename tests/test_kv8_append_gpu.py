@@ -154,6 +154,22 @@ def test_fresh_prompts(dtype, dim, heads, kv_heads, page):
     check(C, new, rule=(angles(128, dim), (dim // 2,), False))
 
 
+@pytest.mark.parametrize("dim", [64, 256])
+def test_more_than_64_sequences(dim):
+    """Blocks are found over groups of sequences, some of which have no tokens."""
+    lens = [(31 * b * b) % 90 + 1 for b in range(150)]
+    new = [0 if b % 6 == 2 else min(n, 1 + (11 * b) % 40) for b, n in enumerate(lens)]
+    C = Cache8(dim, lens, 2, 1, dim, 16, torch.float16)
+    for b, n in enumerate(lens):  # older positions are finite codes of sane exponents
+        used = C.table[b, :(n + 15) // 16].long()
+        for pages, exps in ((C.k, C.ke), (C.v, C.ve)):
+            pages[used] = (C.normal(len(used), 1, 16, dim) * 100).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+            exps[used] = 119 + b % 3
+    check(C, new, rule=(angles(128, dim), (dim // 2,), False))
+    C.lens_list = [n for n in lens]
+    check(C, [1] * 150, starts=False)
+
+
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("dim,rot,sections,interleaved", [(64, 64, (32,), False), (128, 64, (32,), True), (128, 128, (20, 24, 20), False),
                                                           (256, 16, (8,), False), (256, 256, (50, 78), True), (64, 48, (24,), False)])

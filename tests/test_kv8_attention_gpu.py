@@ -151,6 +151,34 @@ def test_decode_first_hides_leading_positions_whatever_they_hold(dim):
     assert bool((out[3] == 0).all()) and bool((out[5] == 0).all())
 
 
+@pytest.mark.parametrize("dim,kv_heads,heads,seqs", [(64, 4, 8, 130), (128, 3, 6, 200), (256, 5, 5, 65), (128, 8, 8, 64)])
+def test_decode_of_many_sequences_longest_first(dim, kv_heads, heads, seqs):
+    """Whole rows by their lengths, in groups of 64: equal lengths, none, one far longer than the others."""
+    lens = [(37 * b * b) % 211 if b % 5 else 96 for b in range(seqs)]
+    lens[seqs // 2], lens[-1], lens[0] = 1900, 0, 1
+    check_decode(Problem8(seqs, lens, heads, kv_heads, dim, 32, torch.float16), bound_len=2100)
+
+
+def test_two_streams_at_once_with_workspaces_of_their_own():
+    P, Q = Problem8(71, [9000], 8, 2, 128, 64, torch.bfloat16), Problem8(72, [700, 5000], 8, 2, 128, 64, torch.bfloat16)
+    attn = tman.Attn(8, 0.09)
+    calls = []
+    for X in (P, Q):
+        B, n = len(X.lens_list), max(X.lens_list)
+        q = X.normal(B, 8, 128)
+        want, got = torch.empty_like(q), torch.empty_like(q)
+        spaces = [torch.zeros(tman.tman_attn_decode_kv8_workspace_bytes(X.cache, attn, n), dtype=torch.uint8, device=dev()) for _ in range(2)]
+        tman.tman_attn_decode_kv8(X.cache, attn, q, X.lens, want, n, spaces[0])
+        calls.append((tman.bound_attn_decode_kv8(X.cache, attn, q, X.lens, got, n, spaces[1]), torch.cuda.Stream(), want, got))
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for call, stream, _, _ in calls:
+            call(stream.cuda_stream)
+    torch.cuda.synchronize()
+    for _, _, want, got in calls:
+        assert torch.equal(want, got)  # the same bits every time
+
+
 @pytest.mark.parametrize("dim,kv_heads,heads", [(128, 1, 1), (64, 2, 8), (256, 1, 4)])
 def test_decode_long_lengths_in_many_pieces(dim, kv_heads, heads):
     P = Problem8(21, [20000, 1, 8191], heads, kv_heads, dim, 64, torch.bfloat16)
@@ -210,6 +238,21 @@ def test_many_rows(dtype, dim, heads, kv_heads, page, mask):
     first, end = mask_of(mask, lens, new)
     P = Problem8(dim, lens, heads, kv_heads, dim, page, dtype)
     check_prefill(P, new, first, end, sample=range(0, 1100, 97))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("many", [False, True])
+def test_prompts_of_more_than_64_sequences(dim, many):
+    lens = [(29 * b * b) % 150 + (b % 3 > 0) for b in range(140)]
+    if many:
+        lens[70] = 2600
+    new = [0 if b % 7 == 3 else min(n, 1 + (13 * b) % (400 if many else 9)) for b, n in enumerate(lens)]
+    if many:
+        new = [min(n, 600) if b == 70 else n for b, n in enumerate(lens)]
+        heads, kv_heads = 24, 1
+    else:
+        heads, kv_heads = 4, 2
+    check_prefill(Problem8(dim, lens, heads, kv_heads, dim, 16, torch.float16), new, sample=[0, 99])
 
 
 @pytest.mark.parametrize("rule", [dict(cap=20.0), dict(sloped=True), dict(window=1), dict(window=100, sloped=True), dict(window=5000), dict(scale=-0.3),
