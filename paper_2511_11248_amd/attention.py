@@ -464,11 +464,18 @@ def _plan_args(where, page_table, page, lens, more, free_pages, free_left, new_l
         n_tokens = given.numel()
     if slots is not None and (slots.dtype is not _int64 or slots.numel() != n_tokens or not slots.is_contiguous()):
         raise TmanError(_ERR_SHAPE, where)
-    return (page_table.data_ptr(), B, wide, page, _ints(lens, B, where), _ints(more, B, where), free_pages.data_ptr(), stack[0],
-            _ints(free_left, 1, where), n_tokens, _ints(new_lens, B, where), _ints(new_left, 1, where), _ints(q_start, B + 1, where),
-            None if slots is None else slots.data_ptr(), None if positions is None else _ints(positions, n_tokens, where),
-            None if owners is None else _ints(owners, n_tokens, where), None if workspace is None else workspace.data_ptr(),
-            0 if workspace is None else workspace.nbytes)
+    i32 = _int32
+    # what _ints would check of each, in one expression (a call of a few microseconds)
+    if lens is None or more is None or free_left is None or new_lens is None or new_left is None or q_start is None or not (
+            lens.dtype is more.dtype is free_left.dtype is new_lens.dtype is new_left.dtype is q_start.dtype is i32
+            and lens.numel() == more.numel() == new_lens.numel() == B and free_left.numel() == new_left.numel() == 1
+            and q_start.numel() == B + 1 and lens.is_contiguous() and more.is_contiguous() and new_lens.is_contiguous()
+            and q_start.is_contiguous()):
+        raise TmanError(_ERR_NULL if any(t is None for t in (lens, more, free_left, new_lens, new_left, q_start)) else _ERR_SHAPE, where)
+    return (page_table.data_ptr(), B, wide, page, lens.data_ptr(), more.data_ptr(), free_pages.data_ptr(), stack[0], free_left.data_ptr(),
+            n_tokens, new_lens.data_ptr(), new_left.data_ptr(), q_start.data_ptr(), None if slots is None else slots.data_ptr(),
+            None if positions is None else _ints(positions, n_tokens, where), None if owners is None else _ints(owners, n_tokens, where),
+            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
 
 
 def tman_kv_plan(page_table, page: int, lens, more, free_pages, free_left, new_lens, new_left, q_start, slots=None, positions=None,

@@ -198,3 +198,28 @@ def test_a_bound_call_keeps_its_tensors(bind, used):
     del call
     gc.collect()
     assert [name for name, ref in alive.items() if ref() is not None] == []
+
+
+def _plan_tensors(B=3, pages=4, n=8):
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    return dict(page_table=ints(B, pages), page=16, lens=ints(B), more=ints(B), free_pages=ints(9), free_left=ints(1), new_lens=ints(B),
+                new_left=ints(1), q_start=ints(B + 1), slots=torch.zeros(n, dtype=torch.int64), positions=ints(n), owners=ints(n))
+
+
+@pytest.mark.parametrize("name,bad,status", [
+    *((n, None, NULL) for n in ("page_table", "lens", "more", "free_pages", "free_left", "new_lens", "new_left", "q_start")),
+    *((n, torch.zeros(3), SHAPE) for n in ("lens", "more", "free_pages", "free_left", "new_lens", "new_left", "q_start", "slots", "positions", "owners")),
+    ("page_table", torch.zeros(3, 4), SHAPE), ("page_table", torch.zeros(12, dtype=torch.int32), SHAPE),
+    ("lens", torch.zeros(4, dtype=torch.int32), SHAPE), ("q_start", torch.zeros(3, dtype=torch.int32), SHAPE),
+    ("more", torch.zeros(6, dtype=torch.int32)[::2], SHAPE), ("q_start", torch.zeros(8, dtype=torch.int32)[::2], SHAPE),
+    ("positions", torch.zeros(7, dtype=torch.int32), SHAPE), ("slots", torch.zeros(8, dtype=torch.int32), SHAPE), ("page", 24, CACHE),
+])
+def test_tensors_that_are_no_plan(name, bad, status):
+    for call in (lambda **a: tman.tman_kv_plan(stream=0, **a), tman.bound_kv_plan):
+        if call is tman.bound_kv_plan and name == "page":
+            continue  # (the library's own checks come with the call)
+        with pytest.raises(tman.TmanError) as e:
+            call(**{**_plan_tensors(), name: bad})
+        assert e.value.status == status
+    with pytest.raises(tman.TmanError):
+        tman.tman_kv_plan(stream=0, **{**_plan_tensors(), "slots": None, "positions": None, "owners": None})
