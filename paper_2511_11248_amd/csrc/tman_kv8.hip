@@ -174,7 +174,10 @@ __device__ __forceinline__ void append_block(const Append8Args& x, int run, int 
             if constexpr (NORM) {
                 if (!value) {
                     size[p] = inverse_size<D>(f[p], a.eps);
-                    if (__any(size[p] < 0x1p-60f)) {  // what a weight could take out of fp32
+                    // The factor waits for the last product, with the block's (2^-120 to 2^117), where no product on the way can leave fp32 before
+                    // the result does: from 1 to 2^10.  Elsewhere, in large rows and in zeros beside a small eps, it comes first.  (Always first:
+                    // 8193 tokens of 3 x 32 heads 86.0 -> 87.7 us.)
+                    if (__any(size[p] < 1.f || size[p] > 0x1p10f)) {
 #pragma unroll
                         for (int z = 0; z < 16; ++z) f[p][z] *= size[p];
                         size[p] = 1.f;
