@@ -596,7 +596,7 @@ int tman_kv8_append(const tman_kv8_cache_t *cache, const tman_head_norm_t *norm,
  * workspace rules (a workspace may go between all four functions).  No weights are accumulated.  Prompts of many rows are
  * attended over a copy of the sequences' values in `type`, which lies in the workspace (2 * n_seqs * max_len * kv_heads * dim
  * elements) as long as it takes at most TMAN_KV8_COPY_BYTES; beyond that the codes are read for every 32 rows, which takes
- * longer: a tight max_len helps.
+ * longer: a tight max_len helps.  A sequence without a token in the call is not looked at, whatever its length and its pages.
  */
 #define TMAN_KV8_COPY_BYTES ((size_t)16 << 30)
 size_t tman_attn_decode_kv8_workspace_bytes(const tman_kv8_cache_t *cache, const tman_attn_t *attn, int32_t max_len);

@@ -284,7 +284,8 @@ void launch_append(const Append8Args& x, int grid, hipStream_t st) {
 // ---- the values of sequences in their type
 //
 // A wave takes a block of a head's keys or values: its codes lie one behind another, and so do its values.  What no token of a sequence
-// can see any more (a window's) is left out; the last tile of 64 positions is filled up with zeros.
+// can see (all of one that has no token in the call, what lies ahead of a window) is left out; the last tile of 64 positions is filled up
+// with zeros.
 constexpr int kUnpackWaves = 4;
 constexpr int kTilePositions = 64;  // what attention reads whole
 
@@ -293,14 +294,16 @@ __global__ __launch_bounds__(kUnpackWaves * 64) void kv8_unpack_kernel(UnpackArg
     constexpr int kPasses = kBlock * D / 1024;
     const int lane = threadIdx.x & 63, wave = scalar((int)threadIdx.x >> 6);
     const int G = a.from.kv_heads, b = blockIdx.z, j0 = (int)blockIdx.x * kBlock;
-    const int len = checked_length(a.from, a.lens, b, a.max_len);
     const int entry = j0 >> a.from.page_shift, to_id = b * a.to.max_pages + entry, slot = j0 & ((1 << a.from.page_shift) - 1);
     if (slot == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.table[to_id] = to_id;
+    // its tokens, as the attention counts them
+    const int start = min(max(scalar_load(a.q_start, b), 0), a.n_tokens), tokens = min(max(scalar_load(a.q_start, b + 1), start), a.n_tokens) - start;
+    if (tokens == 0) return;
+    const int len = checked_length(a.from, a.lens, b, a.max_len);
     const int which = (int)blockIdx.y * kUnpackWaves + wave;  // keys, then values, head after head
     if (j0 >= (len + kTilePositions - 1) / kTilePositions * kTilePositions || which >= 2 * G) return;
     if (a.window > 0) {
-        const int tokens = scalar_load(a.q_start, b + 1) - scalar_load(a.q_start, b);
-        const int64_t least = (int64_t)len - max(tokens, 0) + 1 - a.window;
+        const int64_t least = (int64_t)len - tokens + 1 - a.window;
         if (j0 + kTilePositions <= least) return;
     }
     const bool value = which >= G;
