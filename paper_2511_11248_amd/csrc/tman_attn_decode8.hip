@@ -254,16 +254,16 @@ void launch_tiles(const DecodeArgs& a, const Exps& e, dim3 grid, hipStream_t st)
 //   * Eight waves otherwise, with 4 kB of keys and of values under way each (heads of 256: 8 kB).  Against four with twice that: 32 ragged
 //     sequences of up to 4096 104 and 108 us, 16 of up to 16384 59 and 76, 8 of up to 2000 9.4 and 10.3; heads of 64, two of 262144 103 and
 //     129; heads of 256, 16 of up to 8192 59 and 71.
-//   * Long pieces of few rows, which end together, are read faster by four waves in whole 8 kB (two sequences of 131072: 94 and 102 us);
-//     heads of 64 and 256 are not.
-constexpr int kLongPiece = 256, kManyPieces = 16;  // (in 32 positions)
+//   * Four waves in whole 8 kB read long pieces (128 products' positions and more, pages of 64 to 256) faster where all sequences are as long
+//     as the bound (two of 131072: 89.6 us against 96.9, one of 262144 91 and 98), no faster in pages of 32 and 1024 or with four heads and
+//     fewer in all, slower in pages of 16 (111 and 104), and far slower where lengths differ and units are left with one workgroup (131072 and
+//     a quarter of it: 82 and 65; eight of up to 32768: 80 and 63).  The host knows the bound alone, so there are eight everywhere.
 template <class T>
 void launch_of(const DecodeArgs& a, const Exps& e, dim3 grid, hipStream_t st) {
-    const bool one_each = a.p.split_tiles <= 4, long_pieces = a.p.split_tiles >= kLongPiece && a.p.n_split >= kManyPieces;
+    const bool one_each = a.p.split_tiles <= 4;
     if (a.c.dim == 64) one_each ? launch_tiles<T, 64, 32, 4>(a, e, grid, st) : launch_tiles<T, 64, 64, 8>(a, e, grid, st);
     else if (a.c.dim == 256) one_each ? launch_tiles<T, 256, 32, 4>(a, e, grid, st) : launch_tiles<T, 256, 32, 8>(a, e, grid, st);
-    else if (one_each) launch_tiles<T, 128, 32, 4>(a, e, grid, st);
-    else long_pieces ? launch_tiles<T, 128, 64, 4>(a, e, grid, st) : launch_tiles<T, 128, 32, 8>(a, e, grid, st);
+    else one_each ? launch_tiles<T, 128, 32, 4>(a, e, grid, st) : launch_tiles<T, 128, 32, 8>(a, e, grid, st);
 }
 
 }  // namespace
