@@ -15,7 +15,7 @@
 //   * Only tiles in which some query of a wave does not see all keys compare positions.  There a hidden value may be anything,
 //     infinity and NaN included: such tiles are looked through, and what is not finite is left out of the products and added
 //     where it is seen.
-// Registers: heads of 128 with a distance bias spill 4, no others any.  Tiles that compare positions run without products beside their
+// Registers: none are spilled.  Tiles that compare positions run without products beside their
 // exponentials: documents of 500 positions take 2.4 times their floor.
 // Measured and not better: 8 waves and 256 rows a workgroup (equal), tiles in a rising and a falling order (equal), issue priorities
 // (5 % slower), three workgroups a unit for heads of 64 (equal; 6 % slower on long caches).  Without the requests for keys and
@@ -145,9 +145,11 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     const uint32_t k_ask = ask_row * kRowBytes + (in_row ^ R::key_turn(wave * kOwnRows + ask_row)) * 16;
     const uint32_t v_ask = ask_row * kRowBytes + (in_row ^ R::value_turn32(wave * kOwnRows + ask_row)) * 16;
     // With a distance bias the scores of a causal row rise by up to 64 slopes a tile, so the reference would be set anew, and all sums multiplied,
-    // with nearly every tile: there the tiles are taken from the last one down (8192 tokens of 32 heads over 8 600 -> 520 us, capped 711 -> 632;
-    // heads of 256, 16 over 4, 1007 -> 702, capped 1097 -> 791).
-    auto place_of = [&](int t) { return SLOPED ? t0 + t1 - 1 - t : t; };
+    // with nearly every tile: there the tiles are taken from the last one down (8192 tokens of 32 heads over 8 580 -> 535 us, capped 693 -> 648).  A
+    // bias below zero, which raises them with the distance, has its largest ones in front (528, from the last one down 578).  The first of the key-value
+    // head's biases decides for all.
+    const bool down = SLOPED && scalar(a.slopes[hk * a.group] >= 0.f) != 0;
+    auto place_of = [&](int t) { return down ? t0 + t1 - 1 - t : t; };
     auto find = [&](int t) {
         const int j = place_of(t) * kTile + wave * kOwnRows;
         return row_place(a.c, checked_page(a.c, b, j >> a.c.page_shift, j < len), hk, j) * kRowBytes;
@@ -379,7 +381,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void attn_prefill_kerne
     // positions are compared.  Waves pass the same number of barriers, whichever loop they are in.
     const int whole_hi = kOnlyBehind ? min(inner_hi - 1, least_at) + 1 : inner_hi;
     const int low = min(max((inner_lo + kTile - 1) / kTile, t0), t1), high = min(max(whole_hi / kTile, low), t1);
-    const int whole0 = SLOPED ? t0 + t1 - high : low, whole1 = SLOPED ? t0 + t1 - low : high;
+    const int whole0 = down ? t0 + t1 - high : low, whole1 = down ? t0 + t1 - low : high;
     int t = t0, stop = whole0;
     auto one = [&](auto part) {
         enter(t);
