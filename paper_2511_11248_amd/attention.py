@@ -105,6 +105,8 @@ class KvCache:
     """``tman_kv_cache_t`` over tensors: k_pages, v_pages [n_pages][kv_heads][page][dim] (fp16 or bf16, contiguous), page_table
     int32 [n_seqs][max_pages].  Keeps the tensors alive; holds no state of its own."""
 
+    _codes = False  # (looked at in every call: 0.1 us less than isinstance in a call of its own)
+
     def __init__(self, k_pages, v_pages, page_table):
         where = "KvCache"
         if not _types:
@@ -141,6 +143,8 @@ class KvCache8(KvCache):
     k_exps, v_exps uint8 [n_pages][kv_heads][page / 16], page_table int32 [n_seqs][max_pages]; dtype (fp16 or bf16) of queries, new
     keys and values, and outputs.  Keeps the tensors alive; holds no state of its own."""
 
+    _codes = True
+
     def __init__(self, k_pages, v_pages, k_exps, v_exps, page_table, dtype):
         where = "KvCache8"
         if not _types:
@@ -158,10 +162,6 @@ class KvCache8(KvCache):
         self._c = _CCache8(_CCache(_ptr(k_pages), _ptr(v_pages), _ptr(page_table), n_pages, self.n_seqs, self.max_pages, self.kv_heads,
                                    self.page, self.dim, kind), _ptr(k_exps), _ptr(v_exps))
         self._ref = C.byref(self._c)
-
-
-def _of_16_bits(cache, where: str) -> None:
-    _wants(not isinstance(cache, KvCache8), where, _ERR_CACHE)
 
 
 def _of_8_bits(cache, where: str) -> None:
@@ -258,7 +258,8 @@ def tman_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, po
     """Rotates q and k (q_out may be q; both None: no queries) and writes k and v [n_tokens][kv_heads][dim] into the cache as the
     last positions of their sequences; q_start None: one token a sequence.  k and v have the same distance between tokens."""
     where = "tman_rope_append"
-    _of_16_bits(cache, where)
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, where)
     L = _functions or _load()
     _check(L.tman_rope_append(*_append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights), _stream(stream)), where)
 
@@ -267,7 +268,8 @@ def bound_rope_append(cache: KvCache, q, k, v, lens, q_out, rope: Rope = None, p
     """The same, checked and marshalled once for calls that run every step with the same tensors: call(stream_handle).  The call keeps
     the tensors and handles alive."""
     where = "tman_rope_append"
-    _of_16_bits(cache, where)
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, where)
     fn, args = _load().tman_rope_append, _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights)
 
     def call(stream_handle):
@@ -288,7 +290,8 @@ def tman_norm_rope_append(cache: KvCache, norm: HeadNorm, q, k, v, lens, q_out, 
                           weights=None, stream=None) -> None:
     """tman_rope_append with the norm of query and key heads in the same pass."""
     where = "tman_norm_rope_append"
-    _of_16_bits(cache, where)
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, where)
     _wants(norm is not None, where, _ERR_NULL)
     L = _functions or _load()
     args = _append_args(where, cache, q, k, v, lens, q_out, rope, positions, q_start, weights)
@@ -320,7 +323,8 @@ def bound_kv8_append(cache: KvCache8, q, k, v, lens, q_out, norm: HeadNorm = Non
 
 
 def tman_attn_decode_workspace_bytes(cache: KvCache, attn: Attn, max_len: int, weights: bool = False) -> int:
-    _of_16_bits(cache, "tman_attn_decode_workspace_bytes")
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, "tman_attn_decode_workspace_bytes")
     return int(_load().tman_attn_decode_workspace_bytes(cache._ref, attn._ref, max_len, 1 if weights else 0))
 
 
@@ -337,7 +341,8 @@ def tman_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, wor
                      stream=None) -> None:
     """Attention of one new token of every sequence over its cache; the workspace is zero-filled once by the caller."""
     where = "tman_attn_decode"
-    _of_16_bits(cache, where)
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, where)
     L = _functions or _load()
     _check(L.tman_attn_decode(*_decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights), _stream(stream)), where)
 
@@ -346,7 +351,8 @@ def bound_attn_decode(cache: KvCache, attn: Attn, q, lens, out, max_len: int, wo
     """The same, checked and marshalled once; max_len bounds the lengths of all the steps: call(stream_handle).  The call keeps the
     tensors and handles alive."""
     where = "tman_attn_decode"
-    _of_16_bits(cache, where)
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, where)
     fn, args = _load().tman_attn_decode, _decode_args(where, cache, attn, q, lens, out, max_len, workspace, first, lse, weights)
 
     def call(stream_handle):
@@ -389,17 +395,18 @@ def bound_attn_decode_kv8(cache: KvCache8, attn: Attn, q, lens, out, max_len: in
 
 
 def tman_attn_prefill_workspace_bytes(cache: KvCache, attn: Attn, n_tokens: int, max_len: int) -> int:
-    _of_16_bits(cache, "tman_attn_prefill_workspace_bytes")
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, "tman_attn_prefill_workspace_bytes")
     return int(_load().tman_attn_prefill_workspace_bytes(cache._ref, attn._ref, n_tokens, max_len))
 
 
-def _prefill_args(where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse):
+def _prefill(fn, where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse, stream):
     _wants(q is not None, where, _ERR_NULL)
     n, B, H = q.shape[0], cache.n_seqs, attn.heads
-    return (cache._ref, attn._ref, n, q.data_ptr(), cache._rows(q, where, H, n), _ints(q_start, B + 1, where), _ints(lens, B, where),
-            None if first is None else _ints(first, n, where), None if end is None else _ints(end, n, where), max_len,
-            None if out is None else out.data_ptr(), cache._rows(out, where, H, n), None if lse is None else _floats(lse, n * H, where),
-            None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
+    _check(fn(cache._ref, attn._ref, n, q.data_ptr(), cache._rows(q, where, H, n), _ints(q_start, B + 1, where), _ints(lens, B, where),
+              None if first is None else _ints(first, n, where), None if end is None else _ints(end, n, where), max_len,
+              None if out is None else out.data_ptr(), cache._rows(out, where, H, n), None if lse is None else _floats(lse, n * H, where),
+              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream(stream)), where)
 
 
 def tman_attn_prefill(cache: KvCache, attn: Attn, q, q_start, lens, out, max_len: int, workspace=None, first=None, end=None, lse=None,
@@ -407,10 +414,10 @@ def tman_attn_prefill(cache: KvCache, attn: Attn, q, q_start, lens, out, max_len
     """Attention of the new tokens of prompts over the cache that holds them; token n sees positions first[n] <= j < end[n].  A tight
     max_len makes the call faster."""
     where = "tman_attn_prefill"
-    _of_16_bits(cache, where)
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, where)
     L = _functions or _load()
-    _check(L.tman_attn_prefill(*_prefill_args(where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse),
-                               _stream(stream)), where)
+    _prefill(L.tman_attn_prefill, where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse, stream)
 
 
 def tman_attn_prefill_kv8_workspace_bytes(cache: KvCache8, attn: Attn, n_tokens: int, max_len: int) -> int:
@@ -424,15 +431,15 @@ def tman_attn_prefill_kv8(cache: KvCache8, attn: Attn, q, q_start, lens, out, ma
     where = "tman_attn_prefill_kv8"
     _of_8_bits(cache, where)
     L = _functions or _load()
-    _check(L.tman_attn_prefill_kv8(*_prefill_args(where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse),
-                                   _stream(stream)), where)
+    _prefill(L.tman_attn_prefill_kv8, where, cache, attn, q, q_start, lens, out, max_len, workspace, first, end, lse, stream)
 
 
 def tman_kv_evict(cache: KvCache, weights, lens, keep: int, recent: int, new_table, new_lens, kept, max_len: int, stream=None) -> None:
     """Keeps `keep` positions of every sequence and key-value head (the `recent` last and the largest weights) in the pages of
     new_table; new_lens [n_seqs] (lens itself will do) and kept [n_seqs][kv_heads][keep] receive the lengths and the positions that stayed."""
     where = "tman_kv_evict"
-    _of_16_bits(cache, where)
+    if cache._codes:
+        raise TmanError(_ERR_CACHE, where)
     _wants(weights is not None and new_table is not None, where, _ERR_NULL)
     B = cache.n_seqs
     _wants(new_table.dim() == 2 and new_table.shape[0] == B, where)
