@@ -43,19 +43,25 @@ class ServingBlock:
         self.workspaces = {}
 
     def _workspaces(self, rows):
-        """Of the plan and of the attention, zeroed once."""
+        """Of the plan and of the attention, zeroed once, and the places of the tokens."""
         if rows not in self.workspaces:
             needs = (tman.tman_kv_plan_workspace_bytes(self.seqs, rows), tman.tman_attn_prefill_kv8_workspace_bytes(self.cache, self.attn, rows, self.most))
-            self.workspaces[rows] = [torch.zeros(max(n, 16), dtype=torch.uint8, device=self.lens.device) for n in needs]
+            self.workspaces[rows] = [*(torch.zeros(max(n, 16), dtype=torch.uint8, device=self.lens.device) for n in needs),
+                                     *(torch.zeros(rows, dtype=torch.int32, device=self.lens.device) for _ in range(2))]
         return self.workspaces[rows]
 
     def step(self, x):
-        """x [rows, hidden]: the tokens of self.more, sequence after sequence; rows behind the last granted one are padding.  lens, q_start,
-        the page table and the free pages are up to date afterwards; returns [rows, hidden]."""
+        """x [rows, hidden]: the tokens that self.more asks for, sequence after sequence.  Those of sequences that have to wait are left out, and
+        the others move up: returns [rows, hidden] in the order of q_start, whose rows behind the last token are padding.  lens, q_start, the
+        page table and the free pages are up to date afterwards."""
         rows, h, g, d = x.shape[0], self.heads, self.kv_heads, self.dim
-        plan_space, space = self._workspaces(rows)
+        plan_space, space, positions, owners = self._workspaces(rows)
+        asked, before = self.more.clamp(min=0), self.lens.clone()
         tman.tman_kv_plan(self.table, self.page, self.lens, self.more, self.free_pages, self.free_left, self.lens, self.free_left, self.q_start,
-                          workspace=plan_space, n_tokens=rows)
+                          positions=positions, owners=owners, workspace=plan_space, n_tokens=rows)
+        owner = owners.clamp(min=0).long()
+        source = (asked.cumsum(0) - asked)[owner] + positions - before[owner]
+        x = x[source.clamp(0, rows - 1)]
         qkv = self.qkv(x).view(rows, h + 2 * g, d)
         q, k, v = qkv[:, :h], qkv[:, h:h + g], qkv[:, h + g:]
         tman.tman_kv8_append(self.cache, q, k, v, self.lens, q, norm=self.norm, rope=self.rope, q_start=self.q_start)

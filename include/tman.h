@@ -625,7 +625,8 @@ int tman_attn_prefill_kv8(const tman_kv8_cache_t *cache, const tman_attn_t *attn
  *                 its position and its sequence; -1 behind the last one
  * Tokens of a sequence are granted together or not at all: not where the stack has not enough pages for this sequence and all
  * before it that asked for pages, where the tokens asked for up to it are more than n_tokens, or where its table is too short
- * (which tman_device_status reports).  The caller sees it in q_start.  A length that is out of range is cut to it, `more` below
+ * (which tman_device_status reports).  The caller sees it in q_start: what follows takes the granted tokens' rows, one behind another, so
+ * rows laid out for all that was asked for are gathered by owners and positions.  A length that is out of range is cut to it, `more` below
  * -lens to -lens (reported); pages that the stack has no room for are dropped, and reported.
  *   workspace   : at least tman_kv_plan_workspace_bytes (0: NULL will do), 16-byte aligned, any content
  * Buffers must not overlap but for the two named.  A page must not be twice in what is free and in use.
