@@ -77,19 +77,20 @@ __device__ __forceinline__ float sum_of_head(float x) {
     if constexpr (D >= 256) x = plus_across<0x140>(x);  // eights in rows of 16
     return x;
 }
-// 1 / sqrt(mean x^2 + eps).  Squares of bf16 may leave fp32: then the mean is that of 2^-72 x, beside which eps is nothing.
+// 1 / sqrt(mean x^2 + eps).  Squares of bf16 may leave fp32, and their sum with a large eps too: then the mean is that of 2^-72 x, and eps
+// goes with it.
 template <int D>
 __device__ __forceinline__ float inverse_size(const float (&f)[16], float eps) {
     float sum = 0.f;
 #pragma unroll
     for (int x = 0; x < 16; ++x) sum = __builtin_fmaf(f[x], f[x], sum);
     sum = sum_of_head<D>(sum);
-    if (sum > 1e37f) {
+    if (sum + eps > 1e37f) {
         constexpr float kDown = 0x1p-72f;
         sum = 0.f;
 #pragma unroll
         for (int x = 0; x < 16; ++x) sum = __builtin_fmaf(f[x] * kDown, f[x] * kDown, sum);
-        return __builtin_amdgcn_rsqf(sum_of_head<D>(sum) * (1.f / D)) * kDown;
+        return __builtin_amdgcn_rsqf(__builtin_fmaf(sum_of_head<D>(sum), 1.f / D, eps * kDown * kDown)) * kDown;
     }
     return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.f / D, eps));
 }

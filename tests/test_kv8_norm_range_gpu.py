@@ -6,7 +6,7 @@ import torch
 import kv8_ref as ref
 import paper_2511_11248_amd as tman
 from gpu_helpers import dev
-from test_kv8_append_gpu import Cache8, angles, check
+from test_kv8_append_gpu import F32, Cache8, angles, check
 
 pytestmark = pytest.mark.gpu
 EPS = [1.1920929e-7, 1e-8, 1e-30]
@@ -83,3 +83,26 @@ def test_weights_that_a_large_or_small_key_would_take_out_of_fp32(dim, turned, w
     w = torch.full((dim,), weight, device=dev())
     check(C, [20], norm=tman.HeadNorm(None, w, 1e-20), rule=rule_of(dim, turned), edit=edit, q=False)
     assert not bool(torch.isnan(ref.decode(C.head(C.k, 0, 0, 20)[None], C.head(C.ke, 0, 0, 20)[None])[0, :20]).any())
+
+
+@pytest.mark.parametrize("eps", [1e-6, 1e30, 1e36, 3e38, torch.finfo(torch.float32).max])
+def test_an_eps_beside_squares_that_leave_fp32(eps):
+    """Rows of 1e19 to 3e38 and an eps of their squares' size, into either cache."""
+    x = torch.zeros(4, 3, 64, dtype=torch.bfloat16, device=dev())
+    for i, size in enumerate((1e18, 3e18, 1e19, 3e38)):
+        x[i] = size
+    x[:, :, ::3] *= -0.5
+    pages = torch.zeros(4, 1, 16, 64, dtype=torch.bfloat16, device=dev())
+    table, lens = torch.arange(4, dtype=torch.int32, device=dev())[:, None].contiguous(), torch.ones(4, dtype=torch.int32, device=dev())
+    out = torch.empty(4, 1, 64, dtype=torch.bfloat16, device=dev())
+    norm = tman.HeadNorm(None, None, eps)
+    tman.tman_norm_rope_append(tman.KvCache(pages, torch.zeros_like(pages), table), norm, x[:, :1], x[:, 1:2], x[:, 2:], lens, out)
+    want = ref.normed(x.double(), None, float(torch.tensor(eps, dtype=torch.float32)))
+    for got, h in ((out[:, 0], 0), (pages[:, 0, 0], 1)):
+        assert bool(((got.double() - want[:, h]).abs() <= (2.0 ** -8 + F32) * want[:, h].abs()).all())
+    codes, exps = torch.zeros(4, 1, 16, 64, dtype=torch.uint8, device=dev()), torch.zeros(4, 1, 1, dtype=torch.uint8, device=dev())
+    cache = tman.KvCache8(codes, torch.zeros_like(codes), exps, torch.zeros_like(exps), table, torch.bfloat16)
+    tman.tman_kv8_append(cache, x[:, :1], x[:, 1:2], x[:, 2:], lens, out, norm=norm)
+    got = ref.decode(codes, exps)[:, 0, 0]
+    assert bool(((got - want[:, 1]).abs() <= (2.0 ** -4 + F32) * want[:, 1].abs()).all())
+    assert bool(((out[:, 0].double() - want[:, 0]).abs() <= (2.0 ** -8 + F32) * want[:, 0].abs()).all())
