@@ -8,6 +8,7 @@
 //   * A tile is TILE positions, in products of 32, and a workgroup four or eight waves (see launch_of).
 //   * Keys are read 16 codes at a time, so the two products that they feed take coordinates 64 y + 16 g + 0..7 and + 8..15; the
 //     queries' registers hold the same.  Values come by columns, eight positions a read, which is one operand's.
+//   * Heads of 64 spill 8 or 9 scalar registers, of 256 5 to 8, into vector ones; heads of 128 none.
 #include "tman_attn_join.h"
 #include "tman_codes8_device.h"
 

@@ -15,8 +15,8 @@
 //   * Only tiles in which some query of a wave does not see all keys compare positions.  There a hidden value may be anything,
 //     infinity and NaN included: such tiles are looked through, and what is not finite is left out of the products and added
 //     where it is seen.
-// Registers: none are spilled.  Tiles that compare positions run without products beside their
-// exponentials: documents of 500 positions take 2.4 times their floor.
+// Registers: none are spilled.  Tiles that compare positions run without products beside their exponentials: 8192 tokens in documents of 500
+// positions take 80 us, 2.5 times their floor (heads of 64 63 us, of 256 124: 3.9 times).
 // Measured and not better: 8 waves and 256 rows a workgroup (equal), tiles in a rising and a falling order (equal), issue priorities
 // (5 % slower), three workgroups a unit for heads of 64 (equal; 6 % slower on long caches).  Without the requests for keys and
 // values the loop takes 9 % less.

@@ -3,6 +3,7 @@
 // What bounds it: HBM.  It is built as attn_prefill_few_kernel is (32 rows a workgroup, waves that take tiles in turn through slots of their
 // own, 32x32x16 products with a key a row and a query a column), on codes as in attn_decode8_kernel: they become elements in
 // registers, with the block's power of two; keys are read 16 codes at a time for two products, values by columns of eight positions.
+// Scalar registers are spilled into vector ones: 3 to 6 with heads of 128, 23 to 34 of 64, 20 to 23 of 256.
 #include "tman_attn_join.h"
 #include "tman_codes8_device.h"
 

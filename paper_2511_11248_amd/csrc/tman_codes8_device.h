@@ -61,8 +61,8 @@ __device__ __forceinline__ float load_scale(const uint8_t* exps, int64_t place) 
 // Where a wave's tile of N blocks from position j0 on is (16 positions never leave a page), and the exponents of its blocks, a byte each: few
 // scalar registers, since the next tile's are held beside the present one's.  All pages are asked for before the first is looked at,
 // and all exponents then: two waits, however many blocks.  (Asking for pages a step ahead, and for exponents while the codes are on their
-// way, takes both waits off a wave's path and is no faster: two sequences of 131072 positions 94 -> 98 to 104 us in pages of 64 to 256
-// positions, 105 -> 98 in pages of 16, the others alike.)
+// way, takes both waits off a wave's path and is no faster: two sequences of 131072 positions, with four waves a workgroup, 94 -> 98 to
+// 104 us in pages of 64 to 256 positions, 105 -> 98 in pages of 16, the others alike.)
 template <int N>
 struct TilePlace {
     int id[N];

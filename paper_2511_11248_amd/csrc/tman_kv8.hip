@@ -11,7 +11,8 @@ namespace {
 // The power of two of a block comes from all that is written to it, so a wave takes a block: 16 positions of a head's keys or
 // values, 16 elements a lane and pass, all in registers.  Angles belong to positions, so a wave that takes several heads of a
 // block reads them once, and has the next head's rows on their way.  The queries go to workgroups of their own behind, by token, as for a
-// 16-bit cache: behind, since a block takes longer (8193 tokens of 3 x 32 heads 102 -> 93 us, 4096 of 32 over 8 24.8 -> 20.7).
+// 16-bit cache: behind, since a block takes longer (8193 tokens of 3 x 32 heads 102 -> 93 us, 4096 of 32 over 8 24.8 -> 20.7).  Without a norm
+// heads of 256 spill 118 scalar registers (into vector ones), of 128 9: 2048 tokens of 32 heads of 256 over 8 23.3 us, normed 24.1.
 
 __device__ __forceinline__ uint32_t larger_across(uint32_t x, int y) { return x > (uint32_t)y ? x : (uint32_t)y; }
 __device__ __forceinline__ uint32_t largest_of_wave(uint32_t x) {
